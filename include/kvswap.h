@@ -404,6 +404,142 @@ int kv_pool_tune(kv_pool* p, int32_t what, int64_t value);
 int kv_last_hip_error(const kv_pool* p);
 const char* kv_strerror(int code);
 
+/* ------------------------------------------------------------ operators on the pool's contents
+ * What the model's layers do with the pool between two swaps: keys and values go in (kv_append), the batch's new tokens
+ * attend to what is cached (kv_attn), and the cached tokens that were given least weight go out (kv_evict), which leaves
+ * fewer blocks to swap.  Here the elements of a chunk have a meaning: chunk(l, c, p) is [B][H][D], element d of head h of
+ * token t of the block at byte ((t*H + h)*D + d)*e.  In a pool with scales an fp8 value stands for itself times the fp32
+ * scale of its (layer, K|V, block, head); without, for itself.  D is a multiple of 8, above 128 of 16, and at most 256.
+ *
+ * All calls go to a stream of the caller's (the compute stream), not to the evict or load stream: transfers that touch the same
+ * blocks are ordered by the caller, through wait_event, kv_sync and kv_req_wait.  They are asynchronous, check everything before
+ * they enqueue anything, and read host arrays during the call.  All pointers in the argument structures are device
+ * pointers unless they say otherwise; strides there count elements, the innermost dimension is contiguous.  Queries, keys, values and outputs are of
+ * the batch's io type: KV_F16 or KV_BF16, the pool's own where the pool is of one of these.
+ *
+ * kv_batch: the requests of one step, set once and used by the calls of all layers.  Request i of n has num_tokens[i] tokens
+ * in the cache, the last q_lens[i] of them new in this step: these are the T = sum of q_lens rows of the tensors, request by
+ * request in order.  New token j of request i has cache index num_tokens[i] - q_lens[i] + j; it lives in block
+ * table[index / B] at place index % B.  Tables are CSR as in kv_swap_out; a row may be longer than the tokens need.
+ * A request with num_tokens 0 may still have one row (a padded batch): nothing is stored for it and it sees nothing.
+ * Requests whose tables begin with the same blocks share these: kv_attn reads such a prefix once for all of them. */
+typedef struct kv_batch kv_batch; /* opaque */
+
+/* A batch on the pool; the pool must outlive it (KV_EINVAL: a head_dim that is no multiple of 8, above 128 none of 16, or above 256).
+ * The batch owns device memory for the tables, the plan of the attention
+ * and its partial results, which kv_batch_set allocates as batches grow. */
+int kv_batch_create(kv_pool* p, kv_batch** out);
+/* Waits for the batch's work, then frees it. */
+int kv_batch_destroy(kv_batch* b);
+/* Replaces what the batch describes.  num_q_heads is a multiple of H: query head hq reads KV head hq / (num_q_heads / H).
+ * The copies are enqueued on `stream`; earlier calls with the batch on other streams are waited for on the device, as is the
+ * copy by later calls on other streams.  `stream` must not be capturing; kv_append, kv_attn and kv_evict may be captured on
+ * the stream the batch was set on, and a replay is good until the next kv_batch_set.
+ * Errors: KV_EINVAL (negative sizes, q_lens[i] > num_tokens[i] except 1 row for 0 tokens, a row too short, a head count that does
+ * not fit, a capturing stream), KV_ERANGE (block id): the batch stays as it was; KV_ENOMEM, KV_EHIP: it has no requests. */
+int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens,
+                 const int32_t* q_lens, int32_t num_q_heads, void* stream);
+
+/* What kv_batch_set made of it. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t rows;          /* T */
+  int32_t items;         /* pieces of attention work for one KV head */
+  int32_t partial_rows;  /* rows of partial results for one KV head (0: every row is finished by the one piece that it is in) */
+  int64_t cached_tokens; /* sum of num_tokens */
+  int64_t read_tokens;   /* tokens that attention reads: shared ones once */
+} kv_batch_info;
+int kv_batch_query(const kv_batch* b, kv_batch_info* out);
+
+/* Rotary frequencies for kv_append: turns[j] for the rot/2 pairs is what pair j turns by from one position to the next, in
+ * units of 2^-64 of a turn (a product with a position wraps around by itself, so that no position is too large), and
+ * *magnitude what cosines and sines are multiplied by.  Pair j turns by base^(-2j/rot) radians, scaled:
+ *   KV_ROPE_PLAIN   as it is
+ *   KV_ROPE_LINEAR  divided by factor
+ *   KV_ROPE_BASE    base times factor^(rot/(rot-2))
+ *   KV_ROPE_PARTS   divided by factor where a pair turns at most low times within `trained` positions, as it is from high
+ *                   times on, mixed in between in proportion to the number of turns
+ *   KV_ROPE_YARN    the same with the mix in proportion to the pair's index between those that turn high and low times (rounded
+ *                   outwards), and magnitude 0.1 ln(factor) + 1
+ * Host code, no handle.  KV_EINVAL: rot odd, not positive or above 256, base <= 1, factor < 1, trained <= 0 or high <= low
+ * where they are used. */
+enum { KV_ROPE_PLAIN = 0, KV_ROPE_LINEAR = 1, KV_ROPE_BASE = 2, KV_ROPE_PARTS = 3, KV_ROPE_YARN = 4 };
+int kv_rope_freqs(int32_t rot, double base, int32_t kind, double factor, double trained, double low, double high,
+                  int64_t* turns, float* magnitude);
+
+/* q [T][num_q_heads][D], k and v [T][H][D].  The first rot elements of every head of q and k are turned by position:
+ * pair j, (2j, 2j+1) if interleaved, else (j, j + rot/2), by positions[t] * turns[j] (positions NULL: the cache index; an evicted
+ * cache's positions run ahead of its indices).  The turned q goes to q_out (may be q; neither is used if q is NULL), the turned
+ * k and v into the pool: rounded once from 32 bits.  An fp8 pool takes value / scale[h], beyond +-448 as +-448; with scales,
+ * k_scale and v_scale [H] are stored as the scales of every block that a token goes to: a block's tokens must all have been
+ * stored with the same ones.  Without scales in the pool both are NULL.
+ * Two rows must not have the same place in the pool: requests only append to blocks that they do not share. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layer;
+  int32_t io_dtype;      /* kv_dtype of q, k, v, q_out */
+  int32_t rot;           /* elements turned, even, 0..D */
+  int32_t interleaved;
+  float magnitude;
+  const void* q;         /* nullable */
+  const void* k;
+  const void* v;
+  void* q_out;
+  int64_t q_strides[2], k_strides[2], v_strides[2], q_out_strides[2]; /* per token, per head */
+  const int64_t* turns;  /* [rot/2] */
+  const int32_t* positions; /* [T], nullable */
+  const float *k_scale, *v_scale; /* [H] */
+} kv_append_args;
+int kv_append(kv_batch* b, const kv_append_args* a, void* stream);
+
+/* out[t][hq] = sum over the cached tokens x that row t sees of softmax(scale * q[t][hq] . K[x])[x] * V[x]; new token j of a request
+ * sees its request's tokens up to its own index.  lse[t][hq] (nullable) is the logarithm of the softmax's sum.  A row
+ * that sees nothing has out 0 and lse -inf.  What lies in a block behind a request's last token is never used, whatever it holds.
+ * weights (nullable) [n][H][weights_cap]: weights[i][h][x] += the softmax weights of cached token x of request i, over the request's rows
+ * and the query heads of h; places from num_tokens[i] on stay as they are.
+ * Arithmetic: products of io-type elements (fp8 ones widened exactly) accumulate in 32 bits; softmax and sums in 32 bits. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layer;
+  int32_t io_dtype;
+  float scale;
+  const void* q;
+  void* out;
+  int64_t q_strides[2], out_strides[2]; /* per token, per head */
+  float* lse;
+  int64_t lse_stride;    /* per token */
+  float* weights;
+  int64_t weights_strides[2]; /* per request, per head */
+  int64_t weights_cap;
+} kv_attn_args;
+int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream);
+
+/* For each layer of layer .. layer+num_layers-1, request i and head h, of a request with more than `keep` tokens: kept are its first
+ * keep_first tokens, its last keep_last and of the others those with the largest weights, `keep` in all (a tie goes to the lower
+ * index, a NaN is less than anything).  Their K, V and weights move to indices 0 .. keep-1 in their order, within the request's blocks;
+ * indices that they leave have weight 0.  kept[layer][i][h][0 .. min(keep, num_tokens[i]) - 1] are their former indices.  Requests
+ * with at most `keep` tokens stay (their weights are copied).  Afterwards a request has min(keep, num_tokens[i]) tokens, and the blocks behind
+ * these are free; the batch still describes it as before, so set it again.  In a pool with scales a block takes the
+ * largest scale that its tokens come with, and tokens that come with less are rounded to it.
+ * weights [num_layers][n][H][weights_cap]; weights_out the same (NULL or the same pointer: in place).
+ * req_ids (host, nullable) [n]: requests that the staging arena may hold copies of; their watermark and staged blocks go back to the
+ * blocks that have not changed, and they leave the write queue.
+ * Errors: KV_EINVAL; KV_EDUP: a block that would be written (from index keep_first / B on) is in the batch a second time;
+ * KV_EEXIST: a request of req_ids is swapped out; KV_EHIP. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layer, num_layers;
+  int32_t keep, keep_first, keep_last;
+  const float* weights;
+  float* weights_out;
+  int64_t weights_strides[3]; /* per layer, request, head: of both */
+  int64_t weights_cap;
+  int32_t* kept;
+  int64_t kept_strides[3];
+  const uint64_t* req_ids; /* HOST */
+} kv_evict_args;
+int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream);
+
 /* ------------------------------------------------------------ measurement helpers
  * Ceilings the swap is compared against (the paper prints no bandwidth figure; Section 5.2 only asks that
  * writes use the link fully, so the link's own measured rate is the yardstick); no pool handle needed.  All four are

@@ -10,6 +10,7 @@
 // With KV_STAGING_DEVICE the arena is HBM and the same kernels give the
 // on-device gather/scatter.
 #include "runtime.hip.inc"
+#include "pool_view.hpp"
 
 // Entry of a call that changes state or enqueues work: takes the handle's lock and refuses a handle on which an
 // earlier call failed half-way (KV_EHIP, KV_ENOMEM): its bookkeeping no longer describes what the streams hold.
@@ -1337,3 +1338,42 @@ double kv_bench_link_bidir(void* host_a, const void* dev_a, const void* host_b, 
 }
 
 }  // extern "C"
+
+// ---- what the operators on the pool's contents need of the handle (pool_view.hpp) ----
+namespace kvswap {
+
+int pool_view(kv_pool* p, PoolView* out) {
+  KV_ENTER(p);
+  const kv_pool_config& c = p->cfg;
+  *out = PoolView{c.num_layers, c.num_kv_heads, c.head_dim, c.block_size, c.dtype, c.num_blocks, (char*)c.pool_dev, c.layer_stride,
+                  c.kv_stride, c.block_stride, (float*)c.scale_dev, c.scale_layer_stride / 4, c.scale_kv_stride / 4,
+                  c.scale_block_stride / 4, p->scale_chunk != 0, p->plan_only, p->cu_count};
+  return KV_OK;
+}
+
+int pool_usable(kv_pool* p) { return p->broken ? KV_EHIP : KV_OK; }
+
+void pool_hip_error(kv_pool* p, int code) { p->last_hip = code; }
+
+int pool_may_rewrite(kv_pool* p, int32_t n, const uint64_t* ids) {
+  KV_ENTER(p);
+  for (int32_t i = 0; i < n; i++) {
+    const Req* r = p->planner.find(ids[i]);
+    if (r && r->swapped) return KV_EEXIST;
+  }
+  return KV_OK;
+}
+
+void pool_rewritten(kv_pool* p, int32_t n, const uint64_t* ids, const int32_t* unchanged) {
+  std::lock_guard<std::mutex> g(p->mu);
+  for (int32_t i = 0; i < n; i++) {
+    if (unchanged[i] < 0) continue;
+    p->wq.erase(ids[i]);
+    if (Req* r = p->planner.find_mut(ids[i])) {
+      r->staged = std::min(r->staged, unchanged[i]);
+      r->wm = std::min(r->wm, unchanged[i]);
+    }
+  }
+}
+
+}  // namespace kvswap

@@ -32,13 +32,15 @@ KV_TUNE_KERNEL_EVENTS = 12
 KV_TUNE_HOST_STORES = 13
 KV_TUNE_LINK_IN_WGS, KV_TUNE_LINK_IN_UNROLL = 14, 15
 KV_F16, KV_BF16, KV_FP8_E4M3 = 0, 1, 2
+KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BASE, KV_ROPE_PARTS, KV_ROPE_YARN = 0, 1, 2, 3, 4
 
 EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_swap_out", "kv_swap_out_delta", "kv_swap_in", "kv_evict_and_load", "kv_sync",
            "kv_move_blocks", "kv_move_blocks_noalloc", "kv_req_reserve", "kv_req_release", "kv_req_query", "kv_last_stats",
            "kv_slot_bytes", "kv_last_plan", "kv_pool_tune", "kv_last_hip_error", "kv_strerror",
            "kv_io_stats_get", "kv_budget_blocks", "kv_req_poll", "kv_req_wait", "kv_last_timeline",
            "kv_swap_out_delta_timed", "kv_bench_copy", "kv_bench_copy_scrambled", "kv_bench_link", "kv_bench_link_bidir",
-           "kv_wq_post", "kv_wq_drain", "kv_wq_remove", "kv_wq_pending"]
+           "kv_wq_post", "kv_wq_drain", "kv_wq_remove", "kv_wq_pending",
+           "kv_batch_create", "kv_batch_destroy", "kv_batch_set", "kv_batch_query", "kv_rope_freqs", "kv_append", "kv_attn", "kv_evict"]
 
 
 class kv_pool_config(C.Structure):
@@ -73,6 +75,36 @@ class kv_io_stats(C.Structure):
 
     def as_dict(self):
         return {k: list(getattr(self, k)) for k, _ in self._fields_ if k != "struct_size"}
+
+
+class kv_batch_info(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("items", C.c_int32), ("partial_rows", C.c_int32),
+                ("cached_tokens", C.c_int64), ("read_tokens", C.c_int64)]
+
+    def as_dict(self):
+        return {k: getattr(self, k) for k, _ in self._fields_ if k != "struct_size"}
+
+
+class kv_append_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layer", C.c_int32), ("io_dtype", C.c_int32), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("magnitude", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_out", C.c_void_p), ("q_strides", C.c_int64 * 2), ("k_strides", C.c_int64 * 2), ("v_strides", C.c_int64 * 2),
+                ("q_out_strides", C.c_int64 * 2), ("turns", C.c_void_p), ("positions", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class kv_attn_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layer", C.c_int32), ("io_dtype", C.c_int32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("out", C.c_void_p), ("q_strides", C.c_int64 * 2), ("out_strides", C.c_int64 * 2),
+                ("lse", C.c_void_p), ("lse_stride", C.c_int64), ("weights", C.c_void_p), ("weights_strides", C.c_int64 * 2),
+                ("weights_cap", C.c_int64)]
+
+
+class kv_evict_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layer", C.c_int32), ("num_layers", C.c_int32), ("keep", C.c_int32),
+                ("keep_first", C.c_int32), ("keep_last", C.c_int32), ("weights", C.c_void_p), ("weights_out", C.c_void_p),
+                ("weights_strides", C.c_int64 * 3), ("weights_cap", C.c_int64), ("kept", C.c_void_p), ("kept_strides", C.c_int64 * 3),
+                ("req_ids", C.c_void_p)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -114,6 +146,14 @@ _sig = {
     "kv_wq_drain": (C.c_int, [_vp, C.c_double, _i64, _u32, _vp, _vp, _vp, _vp]),
     "kv_wq_remove": (C.c_int, [_vp, _u64]),
     "kv_wq_pending": (C.c_int, [_vp, _vp, _vp]),
+    "kv_batch_create": (C.c_int, [_vp, C.POINTER(_vp)]),
+    "kv_batch_destroy": (C.c_int, [_vp]),
+    "kv_batch_set": (C.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp]),
+    "kv_batch_query": (C.c_int, [_vp, C.POINTER(kv_batch_info)]),
+    "kv_rope_freqs": (C.c_int, [_i32, C.c_double, _i32, C.c_double, C.c_double, C.c_double, C.c_double, _vp, _vp]),
+    "kv_append": (C.c_int, [_vp, C.POINTER(kv_append_args), _vp]),
+    "kv_attn": (C.c_int, [_vp, C.POINTER(kv_attn_args), _vp]),
+    "kv_evict": (C.c_int, [_vp, C.POINTER(kv_evict_args), _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -508,3 +548,215 @@ class KVPool:
 
     def tune(self, what, value):
         return kv_pool_tune(self.h, what, value)
+
+
+# ------------------------------------------------------------------ operators on the pool's contents
+
+def kv_batch_create(h):
+    """-> (rc, batch handle)"""
+    b = _vp()
+    rc = _lib.kv_batch_create(h, C.byref(b))
+    return rc, b
+
+
+def kv_batch_destroy(b):
+    return _lib.kv_batch_destroy(b)
+
+
+def kv_batch_set(b, offsets, block_ids, num_tokens, q_lens, num_q_heads, stream=None):
+    o, ids, t, q = _i32a(offsets), _i32a(block_ids), _i32a(num_tokens), _i32a(q_lens)
+    if not _rows_ok(len(t), o, ids, q):
+        return KV_EINVAL
+    return _lib.kv_batch_set(b, len(t), _p(o), _p(ids), _p(t), _p(q), int(num_q_heads), stream)
+
+
+def kv_batch_query(b):
+    """-> (rc, dict)"""
+    st = kv_batch_info()
+    st.struct_size = C.sizeof(kv_batch_info)
+    rc = _lib.kv_batch_query(b, C.byref(st))
+    return rc, st.as_dict()
+
+
+def kv_rope_freqs(rot, base=10000.0, kind=KV_ROPE_PLAIN, factor=1.0, trained=0.0, low=1.0, high=4.0):
+    """-> (rc, turns int64[rot/2], magnitude)"""
+    turns, magnitude = np.zeros(max(0, int(rot)) // 2, np.int64), C.c_float(0)
+    rc = _lib.kv_rope_freqs(int(rot), float(base), int(kind), float(factor), float(trained), float(low), float(high),
+                            turns.ctypes.data, C.byref(magnitude))
+    return rc, turns, magnitude.value
+
+
+def kv_append(b, args, stream=None):
+    args.struct_size = C.sizeof(kv_append_args)
+    return _lib.kv_append(b, C.byref(args), stream)
+
+
+def kv_attn(b, args, stream=None):
+    args.struct_size = C.sizeof(kv_attn_args)
+    return _lib.kv_attn(b, C.byref(args), stream)
+
+
+def kv_evict(b, args, stream=None):
+    args.struct_size = C.sizeof(kv_evict_args)
+    return _lib.kv_evict(b, C.byref(args), stream)
+
+
+def kv_check(rc, what="kvswap"):
+    """Raises KVSwapError unless rc is KV_OK."""
+    if rc != KV_OK:
+        raise KVSwapError(rc, what)
+
+
+_IO = {torch.float16: KV_F16, torch.bfloat16: KV_BF16}
+
+
+class KVBatch:
+    """The requests of one step on a KVPool, and the operators on them: append, attn, evict.
+
+    Tensors are torch tensors on the pool's GPU.  q, q_out, out are [T, num_q_heads, D] and k, v [T, H, D], of any strides with
+    a contiguous last dimension; T counts the new tokens of all requests in order.  Calls are enqueued on `stream`
+    (default: torch's current stream of the device) and return the C status codes; shapes, types and devices that the C side cannot
+    see are checked here (KV_EINVAL).
+    """
+
+    def __init__(self, pool):
+        self.pool = pool
+        self.geom = pool.geom
+        self.T, self.Hq, self.n, self.max_len = 0, 0, 0, 0
+        data = pool._keep[0]
+        self.device = data.device if data is not None else None
+        rc, self.h = kv_batch_create(pool.h)
+        if rc:
+            self.h = None
+            raise KVSwapError(rc, "kv_batch_create")
+
+    def close(self):
+        if getattr(self, "h", None):
+            rc = kv_batch_destroy(self.h)
+            self.h = None
+            return rc
+        return KV_OK
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+        return False
+
+    def _alive(self):
+        return self.h and self.pool.h
+
+    def _stream(self, stream):
+        if stream is not None:
+            return stream.cuda_stream
+        return torch.cuda.current_stream(self.device).cuda_stream if self.device is not None else None
+
+    def _rows(self, x, heads, dtype):
+        return x.dtype == dtype and x.device == self.device and x.dim() == 3 and tuple(x.shape) == (self.T, heads, self.geom.D) and x.stride(2) == 1
+
+    def _plain(self, x, dtype, shape):
+        return x.dtype == dtype and x.device == self.device and tuple(x.shape) == shape and (x.dim() == 0 or x.stride(-1) == 1 or shape[-1] <= 1)
+
+    def set(self, offsets, block_ids, num_tokens, q_lens, num_q_heads, stream=None):
+        if not self._alive():
+            return KV_EINVAL
+        t, q = _i32a(num_tokens), _i32a(q_lens)
+        rc = kv_batch_set(self.h, offsets, block_ids, t, q, num_q_heads, self._stream(stream))
+        if rc in (KV_ENOMEM, KV_EHIP):
+            self.T = self.n = self.max_len = 0
+        if rc == KV_OK:
+            self.n, self.T, self.Hq = len(t), int(q.sum()), int(num_q_heads)
+            self.max_len = int(t.max()) if len(t) else 0
+        return rc
+
+    def query(self):
+        rc, st = kv_batch_query(self.h)
+        if rc:
+            raise KVSwapError(rc, "kv_batch_query")
+        return st
+
+    def append(self, layer, q, k, v, q_out=None, turns=None, interleaved=False, magnitude=1.0, positions=None, k_scale=None, v_scale=None, stream=None):
+        """q may be None; q_out defaults to q itself.  turns: int64 [rot/2] on the device (None: nothing is turned), positions: int32 [T]."""
+        if not self._alive():
+            return KV_EINVAL
+        H, dtype = self.geom.H, k.dtype
+        a = kv_append_args()
+        if dtype not in _IO or not self._rows(k, H, dtype) or not self._rows(v, H, dtype):
+            return KV_EINVAL
+        if q is not None:
+            q_out = q if q_out is None else q_out
+            if not self._rows(q, self.Hq, dtype) or not self._rows(q_out, self.Hq, dtype):
+                return KV_EINVAL
+            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
+            a.q_strides[:], a.q_out_strides[:] = q.stride()[:2], q_out.stride()[:2]
+        if turns is not None:
+            if not self._plain(turns, torch.int64, (turns.numel(),)):
+                return KV_EINVAL
+            a.rot, a.turns = 2 * turns.numel(), turns.data_ptr()
+        if positions is not None:
+            if not self._plain(positions, torch.int32, (self.T,)):
+                return KV_EINVAL
+            a.positions = positions.data_ptr()
+        for name, s in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if s is not None:
+                if not self._plain(s, torch.float32, (H,)):
+                    return KV_EINVAL
+                setattr(a, name, s.data_ptr())
+        a.layer, a.io_dtype, a.interleaved, a.magnitude = int(layer), _IO[dtype], bool(interleaved), float(magnitude)
+        a.k, a.v = k.data_ptr(), v.data_ptr()
+        a.k_strides[:], a.v_strides[:] = k.stride()[:2], v.stride()[:2]
+        return kv_append(self.h, a, self._stream(stream))
+
+    def attn(self, layer, q, out, scale, lse=None, weights=None, stream=None):
+        """lse: float32 [T, num_q_heads]; weights: float32 [n, H, cap] with cap no less than the longest request's tokens."""
+        if not self._alive():
+            return KV_EINVAL
+        dtype = q.dtype
+        if dtype not in _IO or not self._rows(q, self.Hq, dtype) or not self._rows(out, self.Hq, dtype):
+            return KV_EINVAL
+        a = kv_attn_args()
+        a.layer, a.io_dtype, a.scale = int(layer), _IO[dtype], float(scale)
+        a.q, a.out = q.data_ptr(), out.data_ptr()
+        a.q_strides[:], a.out_strides[:] = q.stride()[:2], out.stride()[:2]
+        if lse is not None:
+            if not self._plain(lse, torch.float32, (self.T, self.Hq)):
+                return KV_EINVAL
+            a.lse, a.lse_stride = lse.data_ptr(), lse.stride(0)
+        if weights is not None:
+            if weights.dim() != 3 or not self._plain(weights, torch.float32, (self.n, self.geom.H, weights.shape[2])):
+                return KV_EINVAL
+            a.weights, a.weights_cap = weights.data_ptr(), weights.shape[2]
+            a.weights_strides[:] = weights.stride()[:2]
+        return kv_attn(self.h, a, self._stream(stream))
+
+    def evict(self, layer, num_layers, weights, kept, keep, keep_first=0, keep_last=0, weights_out=None, req_ids=None, stream=None):
+        """weights, weights_out (default: weights itself): float32 [num_layers, n, H, cap] of the same strides; kept: int32
+        [num_layers, n, H, keep or more]; req_ids: host uint64 [n]."""
+        if not self._alive():
+            return KV_EINVAL
+        lead = (int(num_layers), self.n, self.geom.H)
+        if weights.dim() != 4 or kept.dim() != 4 or kept.shape[3] < min(keep, self.max_len):
+            return KV_EINVAL
+        if not self._plain(weights, torch.float32, lead + (weights.shape[3],)) or not self._plain(kept, torch.int32, lead + (kept.shape[3],)):
+            return KV_EINVAL
+        a = kv_evict_args()
+        if weights_out is not None:
+            if not self._plain(weights_out, torch.float32, tuple(weights.shape)) or weights_out.stride() != weights.stride():
+                return KV_EINVAL
+            a.weights_out = weights_out.data_ptr()
+        if req_ids is not None:
+            req_ids = _u64a(req_ids)
+            if len(req_ids) != self.n:
+                return KV_EINVAL
+            a.req_ids = req_ids.ctypes.data
+        a.layer, a.num_layers, a.keep, a.keep_first, a.keep_last = int(layer), int(num_layers), int(keep), int(keep_first), int(keep_last)
+        a.weights, a.weights_cap, a.kept = weights.data_ptr(), weights.shape[3], kept.data_ptr()
+        a.weights_strides[:], a.kept_strides[:] = weights.stride()[:3], kept.stride()[:3]
+        return kv_evict(self.h, a, self._stream(stream))
