@@ -16,7 +16,8 @@
 
 namespace kvswap {
 
-// One piece of attention work for one KV head: a tile of rows against a run of keys.
+// One piece of attention work for one KV head: a tile of rows against a run of keys.  Nodes of few rows are tiles of their own (at
+// most kRowTile rows), cut and dealt out to workgroups in even shares of keys; nodes of more rows are cut into big tiles.
 // Row r of a node is new token tokens[first + r / G] with query head r % G of the group.
 struct AttnItem {
   int32_t table;    // where the row of the table begins that names the blocks of the keys
@@ -34,7 +35,11 @@ struct WeightItem {
 struct BatchShape {
   int32_t H = 1, G = 1, B = 1;
   int64_t N = 0;
-  int wgs = 1024;       // workgroups that fill the device
+  int wgs = 512;        // workgroups of row tiles that are to run at a time
+  int least = 512;      // keys below which a run is not cut for their sake
+  int big_wgs = 512;    // the same two for big tiles
+  int big_least = 512;
+  int big_tile = 128;   // rows of a big tile
 };
 
 class BatchPlan {
@@ -44,15 +49,18 @@ class BatchPlan {
   std::vector<int32_t> off, ids, len, q_len, q_first;        // per request (off, q_first: n + 1)
   std::vector<int32_t> tok_req, tok_limit;                   // per row of the tensors: request, keys it sees
   std::vector<int32_t> lists;                                // the nodes' tokens
-  std::vector<AttnItem> items;
+  std::vector<AttnItem> items;                               // first those of row tiles, workgroup by workgroup, then those of big tiles
+  std::vector<int32_t> wg_items;                             // where each workgroup's items begin, and their end
+  int32_t heads = 1;                                         // heads of a workgroup of row tiles: 1, 2 or 4
+  int32_t big_first = 0;                                     // first item of a big tile
   std::vector<int32_t> join_off, join;                       // per token: partial rows of its first query head
   std::vector<WeightItem> witems;
-  int32_t partial_rows = 0;
-  bool mixed = false;  // some item has keys that some of its rows see and others do not
+  int32_t partial_rows = 0, most_parts = 0;
+  bool mixed = false, big_mixed = false;  // some row tile (big tile) has keys that some of its rows see and others do not
 
   // Entries of the table that an item may need: its part of the table is held on chip.
   static constexpr int32_t kMaxEntries = 2048;
-  static constexpr int32_t kTile = 16;  // rows of an item
+  static constexpr int32_t kRowTile = 16;
   static constexpr int32_t kWeightKeys = 512;
 
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
@@ -204,101 +212,175 @@ class BatchPlan {
   }
   static constexpr int64_t kShared = 128;
 
+  struct Tile {
+    int32_t node, list, tokens, row0, rows, limit, clear;
+  };
+  struct Use {
+    int32_t list, tokens, part;  // every row of these tokens has a partial row from here on
+  };
+  std::vector<Tile> few_, big_;
+  std::vector<int32_t> seen_;  // nodes with keys, per token
+  std::vector<Use> uses_;
+
   void cut(const BatchShape& s) {
     lists.clear();
     items.clear();
-    mixed = false;
-    struct Tile {
-      int32_t node, list, row0, rows, limit, clear;
-    };
-    std::vector<Tile> tiles;
-    std::vector<int32_t> seen((size_t)T, 0);  // nodes with keys, per token
+    wg_items.clear();
+    few_.clear();
+    big_.clear();
+    uses_.clear();
+    seen_.assign((size_t)T, 0);
+    mixed = big_mixed = false;
+    partial_rows = 0;
     read = 0;
-    int64_t work = 0;
     for (size_t d = 0; d < nodes_.size(); d++) {
       const Node& node = nodes_[d];
       const int32_t list = (int32_t)lists.size();
       for (int32_t i : node.reqs)
         for (int32_t t = q_first[i]; t < q_first[i + 1]; t++) lists.push_back(t);
       read += node.to - node.from;
-      const int64_t rows = (int64_t)((int32_t)lists.size() - list) * G;
-      for (int64_t r = 0; r < rows; r += kTile) {
-        Tile t{(int32_t)d, list, (int32_t)r, (int32_t)std::min<int64_t>(kTile, rows - r), 0, INT32_MAX};
+      const int32_t tokens = (int32_t)lists.size() - list;
+      const int64_t rows = (int64_t)tokens * G;
+      const int32_t size = rows <= kRowTile ? kRowTile : s.big_tile;
+      for (int64_t r = 0; r < rows; r += size) {
+        Tile t{(int32_t)d, list, tokens, (int32_t)r, (int32_t)std::min<int64_t>(size, rows - r), 0, INT32_MAX};
         for (int64_t j = r / G; j <= (r + t.rows - 1) / G; j++) {
           const int32_t limit = std::min(node.to, tok_limit[lists[list + j]]);
           t.limit = std::max(t.limit, limit);
           t.clear = std::min(t.clear, limit);
         }
-        work += std::max(t.limit - node.from, 0);
-        tiles.push_back(t);
+        (size == kRowTile ? few_ : big_).push_back(t);
       }
       for (size_t j = list; j < lists.size(); j++)
-        if (node.to > node.from) seen[lists[j]]++;
+        if (node.to > node.from) seen_[lists[j]]++;
     }
-    // Equal runs of keys, so many that the device is full.
-    int64_t chunk = (work * s.H + s.wgs - 1) / s.wgs;
-    const int64_t most = std::min<int64_t>((int64_t)(kMaxEntries - 1) * s.B, INT32_MAX / 2) / kStep * kStep;
-    chunk = std::min<int64_t>(most, std::max<int64_t>(kLeast, (chunk + kStep - 1) / kStep * kStep));
-    // Rows that end up in a single piece need no partial results: that holds for a whole node or not at all.
-    std::vector<std::vector<std::pair<int32_t, int32_t>>> parts;  // per node: (partial row of its first row, pieces)
-    partial_rows = 0;
-    std::vector<int32_t> count((size_t)T, 0);
-    struct Use {
-      int32_t list, tokens, part;
-    };
-    std::vector<Use> uses;
-    for (size_t k = 0; k < tiles.size();) {
-      size_t e = k;
-      while (e < tiles.size() && tiles[e].node == tiles[k].node) e++;
-      const Node& node = nodes_[tiles[k].node];
-      int32_t pieces = 1;
-      bool alone = true;
-      for (size_t j = k; j < e; j++)
-        pieces = std::max<int32_t>(pieces, (int32_t)((std::max(tiles[j].limit - node.from, 0) + chunk - 1) / chunk));
-      const int32_t ntok = (tiles[e - 1].row0 + tiles[e - 1].rows) / G;
-      for (int32_t j = 0; j < ntok; j++) alone = alone && seen[lists[tiles[k].list + j]] <= 1;
-      const bool empty = node.to <= node.from;
-      if (empty && !alone_empty(seen, tiles[k].list, ntok)) {  // its rows have all they see at other nodes
-        k = e;
-        continue;
-      }
-      const bool direct = pieces == 1 && alone;
-      // every tile is cut at the same keys, so that partial rows of a piece are a run
-      const int32_t span = node.to - node.from;
-      const int32_t step = pieces > 1 ? (int32_t)(((span + pieces - 1) / pieces + kStep - 1) / kStep * kStep) : span;
-      for (int32_t c = 0; c < pieces; c++) {
-        const int32_t k0 = node.from + (int32_t)std::min<int64_t>(span, (int64_t)c * step);
-        const int32_t k1 = c + 1 < pieces ? node.from + (int32_t)std::min<int64_t>(span, (int64_t)(c + 1) * step) : node.to;
-        if (c && k0 >= k1) break;
-        const int32_t part = direct ? -1 : partial_rows;
-        if (!direct) {
-          partial_rows += ntok * G;
-          uses.push_back({tiles[k].list, ntok, part});
-        }
-        for (size_t j = k; j < e; j++) {
-          const Tile& t = tiles[j];
-          items.push_back({off[node.reqs[0]], k0, std::max(k0, std::min(k1, t.limit)), std::min(k1, t.clear), t.list, t.row0, t.rows,
-                           direct ? -1 : part + t.row0});
-          mixed = mixed || items.back().clear < items.back().k1;
-        }
-      }
-      k = e;
-    }
+    deal_out(s);
+    big_first = (int32_t)items.size();
+    cut_big(s);
+
     join_off.assign((size_t)T + 1, 0);
-    for (const Use& u : uses)
+    for (const Use& u : uses_)
       for (int32_t j = 0; j < u.tokens; j++) join_off[lists[u.list + j] + 1]++;
     for (int32_t t = 0; t < T; t++) join_off[t + 1] += join_off[t];
     join.assign((size_t)join_off[T], 0);
+    most_parts = 0;
+    for (int32_t t = 0; t < T; t++) most_parts = std::max(most_parts, join_off[t + 1] - join_off[t]);
     std::vector<int32_t> at(join_off.begin(), join_off.end() - 1);
-    for (const Use& u : uses)
+    for (const Use& u : uses_)
       for (int32_t j = 0; j < u.tokens; j++) join[at[lists[u.list + j]]++] = u.part + j * G;
   }
-  static constexpr int32_t kLeast = 128, kStep = 128;
+  static constexpr int32_t kStep = 128;  // keys that a workgroup takes at a time
+  static constexpr int64_t kMany = 1024;  // keys of one head a workgroup
 
-  bool alone_empty(const std::vector<int32_t>& seen, int32_t list, int32_t ntok) const {
-    for (int32_t j = 0; j < ntok; j++)
-      if (seen[lists[list + j]] == 0) return true;
-    return false;
+  // Does a tile without keys have something to do?  Only where its rows have no keys at any node.
+  bool idle(const Tile& t) const {
+    if (nodes_[t.node].to > nodes_[t.node].from) return false;
+    for (int32_t j = 0; j < t.tokens; j++)
+      if (seen_[lists[t.list + j]] == 0) return false;
+    return true;
+  }
+  bool alone(const Tile& t) const {
+    for (int32_t j = 0; j < t.tokens; j++)
+      if (seen_[lists[t.list + j]] > 1) return false;
+    return true;
+  }
+  int64_t most_keys(int32_t B) const { return std::min<int64_t>((int64_t)(kMaxEntries - 1) * B, INT32_MAX / 2) / kStep * kStep; }
+
+  void add(const Tile& t, int32_t k0, int32_t k1, int32_t part, bool* any_mixed) {
+    const int32_t end = std::max(k0, std::min(k1, t.limit));
+    items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part});
+    if (items.back().clear < end) *any_mixed = true;
+  }
+
+  // Row tiles.  If one piece of at most `share` keys for each workgroup that the device holds is enough, every tile is cut by itself, and
+  // each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares: a workgroup may take the end
+  // of one tile, whole ones and the beginning of another.
+  void deal_out(const BatchShape& s) {
+    int64_t work = 0;
+    for (const Tile& t : few_) work += std::max(t.limit - nodes_[t.node].from, 0);
+    // Where there is enough for every workgroup, its four wavefronts take four heads (two, if the head count is no multiple of four) rather
+    // than four runs of one head's keys: they then read neighbouring bytes at the same time.  64 requests of 512 to 4096 tokens with 8
+    // heads of 128 in bf16: 106 us instead of 134, 32 requests of 256 to 8192 with 32 heads in fp8: 188 instead of 209.
+    heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
+    const int64_t held = std::max<int64_t>(1, s.wgs * heads / s.H), most = most_keys(s.B);
+    int64_t share = std::max<int64_t>(s.least / heads, (work + held - 1) / held);
+    share = std::min(most, (share + kStep - 1) / kStep * kStep);
+    int64_t pieces = 0;
+    for (const Tile& t : few_) pieces += std::max<int64_t>(1, (std::max(t.limit - nodes_[t.node].from, 0) + share - 1) / share);
+    const bool line = pieces > held;
+    int64_t room = 0;  // keys that the current workgroup still takes
+    for (const Tile& t : few_) {
+      if (idle(t)) continue;
+      const int32_t from = nodes_[t.node].from, keys = std::max(t.limit - from, 0);
+      const bool whole_alone = alone(t);
+      if (!line || keys == 0 || room < kStep) {
+        wg_items.push_back((int32_t)items.size());
+        room = share;
+      }
+      if (!line) {  // equal pieces
+        const int32_t n = (int32_t)std::max<int64_t>(1, (keys + share - 1) / share);
+        const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + kStep - 1) / kStep * kStep);
+        for (int32_t c = 0; c < n && (c == 0 || (int64_t)c * step < keys); c++) {
+          if (c) wg_items.push_back((int32_t)items.size());
+          const int32_t part = n == 1 && whole_alone ? -1 : take_rows(t);
+          add(t, from + c * step, from + (int32_t)std::min<int64_t>(keys, (int64_t)(c + 1) * step), part, &mixed);
+        }
+        continue;
+      }
+      // a rest below half a step is taken along rather than left to another workgroup
+      for (int32_t k = 0; k < keys || keys == 0;) {
+        int32_t n = (int32_t)std::min<int64_t>(keys - k, room);
+        if (keys - k - n < kStep / 2 && keys - k <= most) n = keys - k;
+        const int32_t part = n == keys && whole_alone ? -1 : take_rows(t);
+        add(t, from + k, from + k + n, part, &mixed);
+        k += n;
+        room -= (n + kStep - 1) / kStep * kStep;
+        if (keys == 0) break;
+        if (k < keys) {
+          wg_items.push_back((int32_t)items.size());
+          room = share;
+        }
+      }
+    }
+    wg_items.push_back((int32_t)items.size());
+  }
+  int32_t take_rows(const Tile& t) {
+    const int32_t part = partial_rows;
+    partial_rows += t.rows;  // a row tile has all rows of its tokens
+    uses_.push_back({t.list, t.tokens, part});
+    return part;
+  }
+
+  // Big tiles: all tiles of a node are cut at the same keys, into equal pieces, so many that the device is full.
+  void cut_big(const BatchShape& s) {
+    int64_t work = 0;
+    for (const Tile& t : big_) work += std::max(t.limit - nodes_[t.node].from, 0);
+    int64_t chunk = (work * s.H + s.big_wgs - 1) / s.big_wgs;
+    chunk = std::min(most_keys(s.B), std::max<int64_t>(s.big_least, (chunk + kStep - 1) / kStep * kStep));
+    for (size_t k = 0; k < big_.size();) {
+      size_t e = k;
+      while (e < big_.size() && big_[e].node == big_[k].node) e++;
+      const Node& node = nodes_[big_[k].node];
+      if (idle(big_[k])) {
+        k = e;
+        continue;
+      }
+      const int32_t keys = node.to - node.from, n = (int32_t)std::max<int64_t>(1, (keys + chunk - 1) / chunk);
+      const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + kStep - 1) / kStep * kStep);
+      const bool direct = n == 1 && alone(big_[k]);
+      for (int32_t c = 0; c < n && (c == 0 || (int64_t)c * step < keys); c++) {
+        int32_t part = -1;
+        if (!direct) {
+          part = partial_rows;
+          partial_rows += big_[k].tokens * G;
+          uses_.push_back({big_[k].list, big_[k].tokens, part});
+        }
+        for (size_t j = k; j < e; j++)
+          add(big_[j], node.from + c * step, node.from + (int32_t)std::min<int64_t>(keys, (int64_t)(c + 1) * step), direct ? -1 : part + big_[j].row0,
+              &big_mixed);
+      }
+      k = e;
+    }
   }
 
   void cut_weights() {

@@ -36,7 +36,7 @@ struct kv_batch {
   hipEvent_t up_ev[2] = {nullptr, nullptr};
   bool up_busy[2] = {false, false};
   int turn = 0;
-  const int32_t *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *tok_req = nullptr, *limit = nullptr, *lists = nullptr,
+  const int32_t *wg_items = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *tok_req = nullptr, *limit = nullptr, *lists = nullptr,
                 *join_off = nullptr, *join = nullptr;
   const AttnItem* items = nullptr;
   const WeightItem* witems = nullptr;
@@ -154,15 +154,34 @@ void by_type(const PoolView& v, int32_t io, A... args) {
     fp8 ? by_size(__bf16(), std::true_type()) : by_size(__bf16(), std::false_type());
 }
 
+// Rows of a big tile: what a wavefront's registers hold of their outputs.
+constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }
+
 template <typename E, bool P, int DP>
 struct LaunchAttn {
-  static void go(const AttnArgs* a, int items, bool mixed, hipStream_t st) {
+  static void go(const AttnArgs* a, const BatchPlan* pl, hipStream_t st) {
     constexpr int N = DP / 16;
-    const size_t lds = std::max<size_t>(BatchPlan::kMaxEntries * 4, 2 * 64 * 4 * N * 4 + 2 * 16 * 8);
-    if (mixed)
-      hipLaunchKernelGGL((kv_attn_kernel<E, P, DP, true>), dim3(items * a->H), dim3(256), lds, st, *a);
-    else
-      hipLaunchKernelGGL((kv_attn_kernel<E, P, DP, false>), dim3(items * a->H), dim3(256), lds, st, *a);
+    constexpr size_t table = BatchPlan::kMaxEntries * 4, join = 2 * 64 * 4 * N * 4 + 2 * 16 * 8, keys = 4 * 32 * DP * (P ? 1 : 2);
+    const int wgs = ((int)pl->wg_items.size() - 1) * (a->H / a->hw), big = ((int)pl->items.size() - pl->big_first) * a->H;
+    auto launch = [&](auto kern, int n, const AttnArgs& args, size_t lds) { hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, st, args); };
+    if (wgs) {
+      if (pl->mixed)
+        launch(kv_attn_kernel<E, P, DP, true>, wgs, *a, std::max(table, join));
+      else if (a->kv.D == DP && a->kv.B % 16 == 0)
+        launch(kv_attn_stream_kernel<E, P, DP>, wgs, *a, std::max(keys + table, join));
+      else
+        launch(kv_attn_kernel<E, P, DP, false>, wgs, *a, std::max(table, join));
+    }
+    if (big) {
+      constexpr int C = big_tile(DP) / 64;
+      constexpr size_t lds = 4 * 2 * (DP / 32) * 1024 + 4 * N * 1024 + (P ? 4 * 2 * 32 * 4 : 0) + 16 + table;
+      AttnArgs b = *a;
+      b.items += pl->big_first;
+      if (pl->big_mixed)
+        launch(kv_attn_tile_kernel<E, P, DP, C, true>, big, b, lds);
+      else
+        launch(kv_attn_tile_kernel<E, P, DP, C, false>, big, b, lds);
+    }
   }
 };
 template <typename E, bool P, int DP>
@@ -236,7 +255,11 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   shape.H = b->v.H;
   shape.B = b->v.B;
   shape.N = b->v.N;
-  shape.wgs = b->v.cus * 4;
+  // Two workgroups of row tiles a CU: with three, more places of the pool are read at a time, and each more slowly (64 requests of 512 to
+  // 4096 tokens on 8 heads of 128 in bf16: 106 us with two, 123 with three, 133 with one; 32 of 256 to 8192 on 32 heads in fp8: 189, 190, 246).
+  shape.wgs = b->v.cus * 2;
+  shape.big_wgs = b->v.cus * (b->v.D <= 128 ? 2 : 1);
+  shape.big_tile = big_tile(b->v.D);
   rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, shape);
   if (rc) return rc;
   b->max_len = 0;
@@ -251,7 +274,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     const void** at;
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
-  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
+  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
                         VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.tok_req, b->tok_req), VEC(pl.tok_limit, b->limit),
                         VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
 #undef VEC
@@ -437,6 +460,7 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   AttnArgs k{};
   k.kv = side(b, a->layer);
   k.items = b->items;
+  k.wg_items = b->wg_items;
   k.lists = b->lists;
   k.limit = b->limit;
   k.table = b->table;
@@ -457,17 +481,24 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   k.scale2 = (float)((double)a->scale * 1.4426950408889634);
   k.H = v.H;
   k.G = pl.G;
+  k.hw = pl.heads;
   k.q_vec = aligned(a->q, a->q_strides, 16);
   k.o_vec = aligned(a->out, a->out_strides, 8);
-  by_type<LaunchAttn>(v, a->io_dtype, (const AttnArgs*)&k, (int)pl.items.size(), pl.mixed, st);
+  by_type<LaunchAttn>(v, a->io_dtype, (const AttnArgs*)&k, &pl, st);
   OPCHK(b, hipGetLastError());
   if (pl.partial_rows) {
-    JoinArgs j{b->join_off, b->join, b->part_o, b->part_ml, k.out, k.o_ts, k.o_hs, k.lse, k.lse_ts, v.H, pl.G, v.D, pl.T * v.H * pl.G};
-    const dim3 grid((unsigned)((j.rows + 3) / 4));
-    if (a->io_dtype == KV_F16)
-      hipLaunchKernelGGL((kv_attn_join_kernel<_Float16>), grid, dim3(256), 0, st, j);
-    else
-      hipLaunchKernelGGL((kv_attn_join_kernel<__bf16>), grid, dim3(256), 0, st, j);
+    JoinArgs j{b->join_off, b->join, b->part_o, b->part_ml, k.out, k.o_ts, k.o_hs, k.lse, k.lse_ts, v.H, pl.G, v.D};
+    const dim3 grid((unsigned)pl.T * v.H * pl.G);
+    auto go = [&](auto e) {
+      using E = decltype(e);
+      if (pl.most_parts <= 8)
+        hipLaunchKernelGGL((kv_attn_join_kernel<E, 1>), grid, dim3(64), 0, st, j);
+      else if (pl.most_parts <= 32)
+        hipLaunchKernelGGL((kv_attn_join_kernel<E, 4>), grid, dim3(256), 0, st, j);
+      else
+        hipLaunchKernelGGL((kv_attn_join_kernel<E, 16>), grid, dim3(1024), 0, st, j);
+    };
+    a->io_dtype == KV_F16 ? go(_Float16()) : go(__bf16());
     OPCHK(b, hipGetLastError());
   }
   if (a->weights && !pl.witems.empty()) {

@@ -8,6 +8,7 @@ library raises.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch  # noqa: F401  -- first, so that the library binds to the HIP runtime torch has loaded:
@@ -151,9 +152,9 @@ _sig = {
     "kv_batch_set": (C.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp]),
     "kv_batch_query": (C.c_int, [_vp, C.POINTER(kv_batch_info)]),
     "kv_rope_freqs": (C.c_int, [_i32, C.c_double, _i32, C.c_double, C.c_double, C.c_double, C.c_double, _vp, _vp]),
-    "kv_append": (C.c_int, [_vp, C.POINTER(kv_append_args), _vp]),
-    "kv_attn": (C.c_int, [_vp, C.POINTER(kv_attn_args), _vp]),
-    "kv_evict": (C.c_int, [_vp, C.POINTER(kv_evict_args), _vp]),
+    "kv_append": (C.c_int, [_vp, _vp, _vp]),
+    "kv_attn": (C.c_int, [_vp, _vp, _vp]),
+    "kv_evict": (C.c_int, [_vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -587,18 +588,21 @@ def kv_rope_freqs(rot, base=10000.0, kind=KV_ROPE_PLAIN, factor=1.0, trained=0.0
 
 
 def kv_append(b, args, stream=None):
+    """args: kv_append_args"""
     args.struct_size = C.sizeof(kv_append_args)
-    return _lib.kv_append(b, C.byref(args), stream)
+    return _lib.kv_append(b, C.addressof(args), stream)
 
 
 def kv_attn(b, args, stream=None):
+    """args: kv_attn_args"""
     args.struct_size = C.sizeof(kv_attn_args)
-    return _lib.kv_attn(b, C.byref(args), stream)
+    return _lib.kv_attn(b, C.addressof(args), stream)
 
 
 def kv_evict(b, args, stream=None):
+    """args: kv_evict_args"""
     args.struct_size = C.sizeof(kv_evict_args)
-    return _lib.kv_evict(b, C.byref(args), stream)
+    return _lib.kv_evict(b, C.addressof(args), stream)
 
 
 def kv_check(rc, what="kvswap"):
@@ -608,6 +612,10 @@ def kv_check(rc, what="kvswap"):
 
 
 _IO = {torch.float16: KV_F16, torch.bfloat16: KV_BF16}
+# The argument structures as one packing each, and checks that ask a tensor for as little as possible: the host's share of an append
+# with all its tensors, launch excluded, 5.3 us so, 10.3 with the fields set one by one.
+_APPEND, _ATTN, _EVICT = struct.Struct("@IiiiifPPPPqqqqqqqqPPPP"), struct.Struct("@IiifPPqqqqPqPqqq"), struct.Struct("@IiiiiiPPqqqqPqqqP")
+assert [s.size for s in (_APPEND, _ATTN, _EVICT)] == [C.sizeof(s) for s in (kv_append_args, kv_attn_args, kv_evict_args)]
 
 
 class KVBatch:
@@ -616,19 +624,26 @@ class KVBatch:
     Tensors are torch tensors on the pool's GPU.  q, q_out, out are [T, num_q_heads, D] and k, v [T, H, D], of any strides with
     a contiguous last dimension; T counts the new tokens of all requests in order.  Calls are enqueued on `stream`
     (default: torch's current stream of the device) and return the C status codes; shapes, types and devices that the C side cannot
-    see are checked here (KV_EINVAL).
+    see are checked here (KV_EINVAL).  A batch is used by one thread at a time.
     """
 
     def __init__(self, pool):
         self.pool = pool
         self.geom = pool.geom
-        self.T, self.Hq, self.n, self.max_len = 0, 0, 0, 0
         data = pool._keep[0]
         self.device = data.device if data is not None else None
+        self._dev = data.get_device() if data is not None else -1
+        self._describe(0, 0, 0, 0)
+        self._args = C.create_string_buffer(max(s.size for s in (_APPEND, _ATTN, _EVICT)))
+        self._at = C.addressof(self._args)
         rc, self.h = kv_batch_create(pool.h)
         if rc:
             self.h = None
             raise KVSwapError(rc, "kv_batch_create")
+
+    def _describe(self, n, T, Hq, max_len):
+        self.n, self.T, self.Hq, self.max_len = n, T, Hq, max_len
+        self._q_shape, self._kv_shape = (T, Hq, self.geom.D), (T, self.geom.H, self.geom.D)
 
     def close(self):
         if getattr(self, "h", None):
@@ -650,30 +665,24 @@ class KVBatch:
         self.close()
         return False
 
-    def _alive(self):
-        return self.h and self.pool.h
-
     def _stream(self, stream):
         if stream is not None:
             return stream.cuda_stream
-        return torch.cuda.current_stream(self.device).cuda_stream if self.device is not None else None
+        return torch._C._cuda_getCurrentRawStream(self.device.index) if self.device is not None else None
 
-    def _rows(self, x, heads, dtype):
-        return x.dtype == dtype and x.device == self.device and x.dim() == 3 and tuple(x.shape) == (self.T, heads, self.geom.D) and x.stride(2) == 1
-
-    def _plain(self, x, dtype, shape):
-        return x.dtype == dtype and x.device == self.device and tuple(x.shape) == shape and (x.dim() == 0 or x.stride(-1) == 1 or shape[-1] <= 1)
+    def _fits(self, x, dtype, shape):
+        """Type, device and shape, and a contiguous last dimension."""
+        return x.dtype is dtype and x.shape == shape and x.get_device() == self._dev and (shape[-1] <= 1 or x.stride(-1) == 1)
 
     def set(self, offsets, block_ids, num_tokens, q_lens, num_q_heads, stream=None):
-        if not self._alive():
+        if not self.h or not self.pool.h:
             return KV_EINVAL
         t, q = _i32a(num_tokens), _i32a(q_lens)
         rc = kv_batch_set(self.h, offsets, block_ids, t, q, num_q_heads, self._stream(stream))
         if rc in (KV_ENOMEM, KV_EHIP):
-            self.T = self.n = self.max_len = 0
+            self._describe(0, 0, 0, 0)
         if rc == KV_OK:
-            self.n, self.T, self.Hq = len(t), int(q.sum()), int(num_q_heads)
-            self.max_len = int(t.max()) if len(t) else 0
+            self._describe(len(t), int(q.sum()), int(num_q_heads), int(t.max()) if len(t) else 0)
         return rc
 
     def query(self):
@@ -684,79 +693,76 @@ class KVBatch:
 
     def append(self, layer, q, k, v, q_out=None, turns=None, interleaved=False, magnitude=1.0, positions=None, k_scale=None, v_scale=None, stream=None):
         """q may be None; q_out defaults to q itself.  turns: int64 [rot/2] on the device (None: nothing is turned), positions: int32 [T]."""
-        if not self._alive():
+        dtype, dev, shape, ks, vs = k.dtype, self._dev, self._kv_shape, k.stride(), v.stride()
+        io = _IO.get(dtype)
+        if not (self.h and self.pool.h and io is not None and k.shape == shape and v.shape == shape and v.dtype is dtype and
+                ks[2] == 1 and vs[2] == 1 and k.get_device() == dev and v.get_device() == dev):
             return KV_EINVAL
-        H, dtype = self.geom.H, k.dtype
-        a = kv_append_args()
-        if dtype not in _IO or not self._rows(k, H, dtype) or not self._rows(v, H, dtype):
-            return KV_EINVAL
+        qp, op, qs, qo, rot, tp, pp, kp, vp = 0, 0, (0, 0), (0, 0), 0, 0, 0, 0, 0
         if q is not None:
             q_out = q if q_out is None else q_out
-            if not self._rows(q, self.Hq, dtype) or not self._rows(q_out, self.Hq, dtype):
+            shape, qs, qo = self._q_shape, q.stride(), q_out.stride()
+            if not (q.shape == shape and q_out.shape == shape and q.dtype is dtype and q_out.dtype is dtype and qs[2] == 1 and qo[2] == 1 and
+                    q.get_device() == dev and q_out.get_device() == dev):
                 return KV_EINVAL
-            a.q, a.q_out = q.data_ptr(), q_out.data_ptr()
-            a.q_strides[:], a.q_out_strides[:] = q.stride()[:2], q_out.stride()[:2]
+            qp, op = q.data_ptr(), q_out.data_ptr()
         if turns is not None:
-            if not self._plain(turns, torch.int64, (turns.numel(),)):
+            rot, tp = 2 * turns.numel(), turns.data_ptr()
+            if turns.dtype is not torch.int64 or turns.get_device() != dev or not turns.is_contiguous():
                 return KV_EINVAL
-            a.rot, a.turns = 2 * turns.numel(), turns.data_ptr()
         if positions is not None:
-            if not self._plain(positions, torch.int32, (self.T,)):
+            pp = positions.data_ptr()
+            if positions.dtype is not torch.int32 or positions.shape != (self.T,) or positions.get_device() != dev or not positions.is_contiguous():
                 return KV_EINVAL
-            a.positions = positions.data_ptr()
-        for name, s in (("k_scale", k_scale), ("v_scale", v_scale)):
-            if s is not None:
-                if not self._plain(s, torch.float32, (H,)):
-                    return KV_EINVAL
-                setattr(a, name, s.data_ptr())
-        a.layer, a.io_dtype, a.interleaved, a.magnitude = int(layer), _IO[dtype], bool(interleaved), float(magnitude)
-        a.k, a.v = k.data_ptr(), v.data_ptr()
-        a.k_strides[:], a.v_strides[:] = k.stride()[:2], v.stride()[:2]
-        return kv_append(self.h, a, self._stream(stream))
+        if k_scale is not None:
+            kp = k_scale.data_ptr()
+            if not self._fits(k_scale, torch.float32, (self.geom.H,)):
+                return KV_EINVAL
+        if v_scale is not None:
+            vp = v_scale.data_ptr()
+            if not self._fits(v_scale, torch.float32, (self.geom.H,)):
+                return KV_EINVAL
+        _APPEND.pack_into(self._args, 0, _APPEND.size, layer, io, rot, 1 if interleaved else 0, magnitude, qp, k.data_ptr(), v.data_ptr(), op,
+                          qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], tp, pp, kp, vp)
+        return _lib.kv_append(self.h, self._at, self._stream(stream))
 
     def attn(self, layer, q, out, scale, lse=None, weights=None, stream=None):
         """lse: float32 [T, num_q_heads]; weights: float32 [n, H, cap] with cap no less than the longest request's tokens."""
-        if not self._alive():
+        dtype, dev, shape, qs, os_ = q.dtype, self._dev, self._q_shape, q.stride(), out.stride()
+        io = _IO.get(dtype)
+        if not (self.h and self.pool.h and io is not None and q.shape == shape and out.shape == shape and out.dtype is dtype and
+                qs[2] == 1 and os_[2] == 1 and q.get_device() == dev and out.get_device() == dev):
             return KV_EINVAL
-        dtype = q.dtype
-        if dtype not in _IO or not self._rows(q, self.Hq, dtype) or not self._rows(out, self.Hq, dtype):
-            return KV_EINVAL
-        a = kv_attn_args()
-        a.layer, a.io_dtype, a.scale = int(layer), _IO[dtype], float(scale)
-        a.q, a.out = q.data_ptr(), out.data_ptr()
-        a.q_strides[:], a.out_strides[:] = q.stride()[:2], out.stride()[:2]
+        lp, ls, wp, ws, cap = 0, 0, 0, (0, 0), 0
         if lse is not None:
-            if not self._plain(lse, torch.float32, (self.T, self.Hq)):
+            if not self._fits(lse, torch.float32, (self.T, self.Hq)):
                 return KV_EINVAL
-            a.lse, a.lse_stride = lse.data_ptr(), lse.stride(0)
+            lp, ls = lse.data_ptr(), lse.stride(0)
         if weights is not None:
-            if weights.dim() != 3 or not self._plain(weights, torch.float32, (self.n, self.geom.H, weights.shape[2])):
+            if weights.dim() != 3 or not self._fits(weights, torch.float32, (self.n, self.geom.H, weights.shape[2])):
                 return KV_EINVAL
-            a.weights, a.weights_cap = weights.data_ptr(), weights.shape[2]
-            a.weights_strides[:] = weights.stride()[:2]
-        return kv_attn(self.h, a, self._stream(stream))
+            wp, ws, cap = weights.data_ptr(), weights.stride(), weights.shape[2]
+        _ATTN.pack_into(self._args, 0, _ATTN.size, layer, io, scale, q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], lp, ls, wp,
+                        ws[0], ws[1], cap)
+        return _lib.kv_attn(self.h, self._at, self._stream(stream))
 
     def evict(self, layer, num_layers, weights, kept, keep, keep_first=0, keep_last=0, weights_out=None, req_ids=None, stream=None):
         """weights, weights_out (default: weights itself): float32 [num_layers, n, H, cap] of the same strides; kept: int32
         [num_layers, n, H, keep or more]; req_ids: host uint64 [n]."""
-        if not self._alive():
+        if not self.h or not self.pool.h or weights.dim() != 4 or kept.dim() != 4 or kept.shape[3] < min(keep, self.max_len):
             return KV_EINVAL
-        lead = (int(num_layers), self.n, self.geom.H)
-        if weights.dim() != 4 or kept.dim() != 4 or kept.shape[3] < min(keep, self.max_len):
+        lead, ws, ks, out, ids = (num_layers, self.n, self.geom.H), weights.stride(), kept.stride(), 0, 0
+        if not self._fits(weights, torch.float32, lead + (weights.shape[3],)) or not self._fits(kept, torch.int32, lead + (kept.shape[3],)):
             return KV_EINVAL
-        if not self._plain(weights, torch.float32, lead + (weights.shape[3],)) or not self._plain(kept, torch.int32, lead + (kept.shape[3],)):
-            return KV_EINVAL
-        a = kv_evict_args()
         if weights_out is not None:
-            if not self._plain(weights_out, torch.float32, tuple(weights.shape)) or weights_out.stride() != weights.stride():
+            if not self._fits(weights_out, torch.float32, weights.shape) or weights_out.stride() != ws:
                 return KV_EINVAL
-            a.weights_out = weights_out.data_ptr()
+            out = weights_out.data_ptr()
         if req_ids is not None:
             req_ids = _u64a(req_ids)
             if len(req_ids) != self.n:
                 return KV_EINVAL
-            a.req_ids = req_ids.ctypes.data
-        a.layer, a.num_layers, a.keep, a.keep_first, a.keep_last = int(layer), int(num_layers), int(keep), int(keep_first), int(keep_last)
-        a.weights, a.weights_cap, a.kept = weights.data_ptr(), weights.shape[3], kept.data_ptr()
-        a.weights_strides[:], a.kept_strides[:] = weights.stride()[:3], kept.stride()[:3]
-        return kv_evict(self.h, a, self._stream(stream))
+            ids = req_ids.ctypes.data
+        _EVICT.pack_into(self._args, 0, _EVICT.size, layer, num_layers, keep, keep_first, keep_last, weights.data_ptr(), out,
+                         ws[0], ws[1], ws[2], weights.shape[3], kept.data_ptr(), ks[0], ks[1], ks[2], ids)
+        return _lib.kv_evict(self.h, self._at, self._stream(stream))

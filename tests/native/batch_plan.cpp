@@ -21,7 +21,7 @@
 
 int main(int argc, char** argv) {
   const int seeds = argc > 1 ? atoi(argv[1]) : 400;
-  long shared_nodes = 0, joined = 0, direct = 0;
+  long shared_nodes = 0, joined = 0, direct = 0, dealt = 0;
   for (int seed = 0; seed < seeds; seed++) {
     std::mt19937 rng(seed);
     auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
@@ -32,6 +32,10 @@ int main(int argc, char** argv) {
     const int G = pick(1, 20);
     s.N = 1 << 20;
     s.wgs = pick(0, 1) ? 1024 : pick(1, 64);
+    s.big_tile = pick(0, 1) ? 128 : 64;
+    s.big_wgs = pick(0, 1) ? 512 : pick(1, 64);
+    s.least = pick(0, 1) ? 512 : 128;
+    s.big_least = pick(0, 1) ? 512 : 128;
     const int n = pick(0, 12);
     std::vector<int32_t> off{pick(0, 3)}, ids((size_t)off[0], -7), len, ql;
     int fresh = 0;
@@ -57,7 +61,9 @@ int main(int argc, char** argv) {
     std::map<int, int> part_row;                          // partial row -> row
     std::vector<int> finished((size_t)p.T * G, 0);
     for (const auto& it : p.items) {
-      CHECK(it.rows >= 1 && it.rows <= 64, "rows %d", it.rows);
+      const bool big = &it - p.items.data() >= p.big_first;
+      CHECK(it.rows >= 1 && it.rows <= (big ? s.big_tile : p.kRowTile), "rows %d", it.rows);
+      CHECK(it.clear >= it.k1 || (big ? p.big_mixed : p.mixed), "mixed");
       CHECK(it.k0 >= 0 && it.k1 >= it.k0, "keys %d %d", it.k0, it.k1);
       if (it.k1 > it.k0) {
         const int b0 = it.k0 / s.B, b1 = (it.k1 - 1) / s.B;
@@ -100,6 +106,11 @@ int main(int argc, char** argv) {
         nj ? joined++ : direct++;
       }
     }
+    CHECK((p.heads == 1 || p.heads == 2 || p.heads == 4) && s.H % p.heads == 0, "%d heads of %d", p.heads, s.H);
+    // every row tile's item has its workgroup
+    CHECK(p.wg_items.size() >= 1 && p.wg_items.back() == p.big_first, "workgroups");
+    for (size_t k = 0; k + 1 < p.wg_items.size(); k++) CHECK(p.wg_items[k] < p.wg_items[k + 1] && (k || p.wg_items[0] == 0), "workgroup %zu", k);
+    for (size_t k = 0; k + 1 < p.wg_items.size(); k++) dealt += p.wg_items[k + 1] - p.wg_items[k] > 1;
     int64_t cached = 0;
     for (int i = 0; i < n; i++)
       if (ql[i]) cached += len[i];
@@ -116,8 +127,8 @@ int main(int argc, char** argv) {
       for (auto& k : w[i]) CHECK(k.second == 1 && k.first < len[i], "weight of key %d", k.first);
     }
   }
-  if (!shared_nodes || !joined || !direct) {
-    fprintf(stderr, "the batches do not reach every kind: %ld shared, %ld joined, %ld direct\n", shared_nodes, joined, direct);
+  if (!shared_nodes || !joined || !direct || !dealt) {
+    fprintf(stderr, "the batches do not reach every kind: %ld shared, %ld joined, %ld direct, %ld dealt\n", shared_nodes, joined, direct, dealt);
     return 1;
   }
   printf("plans ok: %ld batches with shared keys, %ld rows joined, %ld finished at once\n", shared_nodes, joined, direct);

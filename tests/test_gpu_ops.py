@@ -98,6 +98,10 @@ ATTN = {
     "d 112": ((1, 2, 112, 4, "f16", False), 16, [130, 65], [3, 1], (), "block", (0, 0)),
     "d 192": ((1, 2, 192, 16, "bf16", False), 2, [400, 31], [1, 4], (), "layer", (0, 0)),
     "d 256": ((1, 1, 256, 20, "f16", False), 8, [500, 41], [2, 1], (), "layer", (0, 0)),
+    "d 256, blocks of 16": ((2, 2, 256, 16, "bf16", False), 4, [300, 37], [1, 1], (), "layer", (0, 0)),
+    "d 64, blocks of 32": ((2, 3, 64, 32, "bf16", False), 16, [1300, 37, 128], [1, 1, 1], (), "block", (0, 0)),
+    "fp8 d 64, blocks of 16": ((2, 3, 64, 16, "fp8_e4m3", True), 5, [1300, 37, 128], [1, 1, 1], (), "block", (0, 0)),
+    "fp8 d 256, blocks of 48": ((2, 2, 256, 48, "fp8_e4m3", True), 3, [700, 37, 128], [1, 1, 1], (), "layer", (0, 0)),
     "d 8": ((1, 2, 8, 8, "bf16", False), 2, [70], [1], (), "layer", (0, 0)),
     "many query heads": ((1, 1, 128, 16, "bf16", False), 71, [290, 45], [1, 2], (), "layer", (0, 0)),
     "long, few rows": ((1, 1, 128, 16, "bf16", False), 8, [20011], [1], (), "layer", (0, 0)),
