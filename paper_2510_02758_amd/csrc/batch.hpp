@@ -32,6 +32,11 @@ struct WeightItem {
   int32_t req, k0, k1, pad;
 };
 
+// Where a new token goes: place `place` of block `block` (-1: nowhere), cache index `index`.
+struct TokenPlace {
+  int32_t block, place, index, pad;
+};
+
 struct BatchShape {
   int32_t H = 1, G = 1, B = 1;
   int64_t N = 0;
@@ -48,6 +53,7 @@ class BatchPlan {
   int64_t cached = 0, read = 0;
   std::vector<int32_t> off, ids, len, q_len, q_first;        // per request (off, q_first: n + 1)
   std::vector<int32_t> tok_req, tok_limit;                   // per row of the tensors: request, keys it sees
+  std::vector<TokenPlace> places;                            // per row
   std::vector<int32_t> lists;                                // the nodes' tokens
   std::vector<AttnItem> items;                               // first those of row tiles, workgroup by workgroup, then those of big tiles
   std::vector<int32_t> wg_items;                             // where each workgroup's items begin, and their end
@@ -128,6 +134,8 @@ class BatchPlan {
     ids.reserve(table);
     tok_req.clear();
     tok_limit.clear();
+    places.clear();
+    places.reserve(rows);
     tok_req.reserve(rows);
     tok_limit.reserve(rows);
     for (int32_t i = 0; i < n_; i++) {
@@ -137,7 +145,9 @@ class BatchPlan {
       q_first.push_back(q_first.back() + q_lens[i]);
       for (int32_t j = 0; j < q_lens[i]; j++) {
         tok_req.push_back(i);
-        tok_limit.push_back(tokens[i] ? tokens[i] - q_lens[i] + j + 1 : 0);
+        const int32_t x = tokens[i] ? tokens[i] - q_lens[i] + j : -1;
+        tok_limit.push_back(x + 1);
+        places.push_back({x < 0 ? -1 : ids[off[i] + x / s.B], x < 0 ? 0 : x % s.B, x, 0});
       }
     }
     n = n_;

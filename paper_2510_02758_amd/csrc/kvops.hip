@@ -20,6 +20,7 @@
 using kvswap::AttnItem;
 using kvswap::BatchPlan;
 using kvswap::PoolView;
+using kvswap::TokenPlace;
 using kvswap::WeightItem;
 
 struct kv_batch {
@@ -36,10 +37,11 @@ struct kv_batch {
   hipEvent_t up_ev[2] = {nullptr, nullptr};
   bool up_busy[2] = {false, false};
   int turn = 0;
-  const int32_t *wg_items = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *tok_req = nullptr, *limit = nullptr, *lists = nullptr,
+  const int32_t *wg_items = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
                 *join_off = nullptr, *join = nullptr;
   const AttnItem* items = nullptr;
   const WeightItem* witems = nullptr;
+  const TokenPlace* places = nullptr;
 
   // Partial results and, for callers that want weights without lse, the lse.
   char* ws = nullptr;
@@ -275,7 +277,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
   const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
-                        VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.tok_req, b->tok_req), VEC(pl.tok_limit, b->limit),
+                        VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
                         VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
 #undef VEC
   size_t need = 0;
@@ -413,10 +415,7 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
   k.positions = a->positions;
   k.k_scale = a->k_scale;
   k.v_scale = a->v_scale;
-  k.tok_req = b->tok_req;
-  k.limit = b->limit;
-  k.off = b->off;
-  k.table = b->table;
+  k.places = b->places;
   k.pool = v.pool + a->layer * v.ls;
   k.vk = v.ks;
   k.bs = v.bs;
@@ -428,14 +427,22 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
   k.H = v.H;
   k.Hq = a->q ? v.H * pl.G : 0;
   k.D = v.D;
-  k.B = v.B;
   k.interleaved = a->interleaved;
-  const bool fp8 = v.dtype == KV_FP8_E4M3;
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(pl.T), dim3(256), 0, st, k); };
-  if (a->io_dtype == KV_F16)
-    fp8 ? go(kv_append_kernel<_Float16, true>) : go(kv_append_kernel<_Float16, false>);
+  const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16;
+  const bool wide = a->rot % (a->interleaved ? 8 : 16) == 0 && aligned(a->k, a->k_strides, 16) && aligned(a->v, a->v_strides, 16) &&
+                    (!a->q || (aligned(a->q, a->q_strides, 16) && aligned(a->q_out, a->q_out_strides, 16)));
+  if (wide) {
+    k.pairs = a->rot / (a->interleaved ? 8 : 16);
+    k.units = k.pairs + (v.D - a->rot) / 8;
+    k.chunks = ((k.Hq + v.H) * k.units + v.H * (v.D / 8) + 255) / 256;
+  }
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)pl.T * (wide ? k.chunks : 1)), dim3(256), 0, st, k); };
+  if (wide)
+    f16 ? (fp8 ? go(kv_append_wide_kernel<_Float16, true>) : go(kv_append_wide_kernel<_Float16, false>))
+        : (fp8 ? go(kv_append_wide_kernel<__bf16, true>) : go(kv_append_wide_kernel<__bf16, false>));
   else
-    fp8 ? go(kv_append_kernel<__bf16, true>) : go(kv_append_kernel<__bf16, false>);
+    f16 ? (fp8 ? go(kv_append_kernel<_Float16, true>) : go(kv_append_kernel<_Float16, false>))
+        : (fp8 ? go(kv_append_kernel<__bf16, true>) : go(kv_append_kernel<__bf16, false>));
   OPCHK(b, hipGetLastError());
   return KV_OK;
 }

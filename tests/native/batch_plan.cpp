@@ -92,6 +92,8 @@ int main(int argc, char** argv) {
     for (int t = 0; t < p.T; t++) {
       const int req = p.tok_req[t], limit = len[req] ? len[req] - ql[req] + (t - p.q_first[req]) + 1 : 0;
       CHECK(limit == p.tok_limit[t], "limit");
+      const auto& at = p.places[t];
+      CHECK(at.index == limit - 1 && at.block == (limit ? ids[off[req] + (limit - 1) / s.B] : -1) && at.place == (limit ? (limit - 1) % s.B : 0), "place");
       const int nj = p.join_off[t + 1] - p.join_off[t];
       for (int g = 0; g < G; g++) {
         const int row = t * G + g;
