@@ -575,10 +575,13 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     hipLaunchKernelGGL(kv_evict_select_kernel, dim3(heads), dim3(kSelectLanes), 0, st, k);
     OPCHK(b, hipGetLastError());
     if (crowded) {
+      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(heads * 2), dim3(256), 0, st, k); };
       if (v.scale)
-        hipLaunchKernelGGL((kv_evict_move_kernel<true>), dim3(heads * 2), dim3(256), 0, st, k);
+        go(kv_evict_move_scaled_kernel<true>);
+      else if (v.D * k.e % 16)
+        go(kv_evict_move_scaled_kernel<false>);
       else
-        hipLaunchKernelGGL((kv_evict_move_kernel<false>), dim3(heads * 2), dim3(256), 0, st, k);
+        go(kv_evict_move_kernel<4>);
       OPCHK(b, hipGetLastError());
     }
   }

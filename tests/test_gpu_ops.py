@@ -458,6 +458,8 @@ EVICT = {
     "last only": ((1, 2, 80, 4, "bf16", False), [90, 55], 17, 0, 17, "random"),
     "all alike": ((2, 3, 128, 16, "bf16", False), [500, 333], 100, 0, 0, "alike"),
     "ties": ((2, 3, 128, 16, "bf16", False), [700, 333], 200, 5, 30, "ties"),
+    "an edge between two values": ((1, 2, 64, 16, "bf16", False), [400], 150, 20, 30, "edge"),
+    "an edge at the lowest": ((1, 2, 64, 16, "bf16", False), [400], 150, 20, 30, "lowest"),
     "zeros of both signs": ((1, 2, 96, 1, "f16", False), [700, 333], 200, 5, 30, "zeros"),
     "special": ((1, 2, 96, 1, "f16", False), [700, 333], 200, 5, 30, "special"),
     "all but one": ((1, 2, 112, 8, "f16", False), [700, 700], 699, 5, 30, "random"),
@@ -480,6 +482,10 @@ def _weights(rng, kind, shape):
         w = np.round(w * 5).astype(np.float32) / 5
     elif kind == "zeros":
         w = np.where(rng.uniform(0, 1, shape) < 0.9, np.float32(0) * np.sign(rng.standard_normal(shape)), w).astype(np.float32)
+    elif kind in ("edge", "lowest"):  # just as many as stay have one value, all others the one below it; the one value is the lowest that there is
+        w[:] = np.nextafter(np.float32(0.5), np.float32(0)) if kind == "edge" else np.nan
+        pick = rng.permutation(np.arange(20, 370))[:100]
+        w[..., pick] = 0.5 if kind == "edge" else np.array(0xFF7FFFFF, np.uint32).view(np.float32)
     elif kind == "special":
         r = rng.uniform(0, 1, shape)
         w = np.where(r < 0.5, np.nan, np.where(r < 0.6, np.inf, np.where(r < 0.7, -np.inf, np.where(r < 0.8, -w, w * 1e-42)))).astype(np.float32)
