@@ -179,6 +179,16 @@ struct LaunchAttn {
       constexpr size_t lds = 4 * 2 * (DP / 32) * 1024 + 4 * N * 1024 + (P ? 4 * 2 * 32 * 4 : 0) + 16 + table;
       AttnArgs b = *a;
       b.items += pl->big_first;
+      if constexpr (!P) {
+        if (a->kv.D == DP && a->kv.B % 16 == 0) {
+          constexpr size_t own = 4 * 64 * DP * 2 + 16 + table;
+          if (pl->big_mixed)
+            launch(kv_attn_big_kernel<E, DP, C, true>, big, b, own);
+          else
+            launch(kv_attn_big_kernel<E, DP, C, false>, big, b, own);
+          return;
+        }
+      }
       if (pl->big_mixed)
         launch(kv_attn_tile_kernel<E, P, DP, C, true>, big, b, lds);
       else
@@ -485,7 +495,9 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   }
   k.part_o = b->part_o;
   k.part_ml = b->part_ml;
-  k.scale2 = (float)((double)a->scale * 1.4426950408889634);
+  // a scale of next to nothing rather than none: what is masked has to stay below everything
+  k.scale2 = (float)std::max(std::fabs((double)a->scale) * 1.4426950408889634, 1e-30);
+  k.flip = a->scale < 0;
   k.H = v.H;
   k.G = pl.G;
   k.hw = pl.heads;

@@ -113,6 +113,8 @@ ATTN = {
     "fp8 d 256": ((2, 1, 256, 16, "fp8_e4m3", True), 4, [100, 511], [40, 1], (), "layer", (0, 0)),
     "prompt from nothing": ((1, 2, 128, 16, "bf16", False), 4, [150], [150], (), "layer", (0, 0)),
     "prompt chunks": ((1, 2, 128, 16, "bf16", False), 4, [600, 70, 333], [130, 70, 1], (), "layer", (0, 0)),
+    "prompt chunk, d 64, blocks of 16": ((1, 3, 64, 16, "f16", False), 2, [600, 300], [290, 77], (), "block", (0, 0)),
+    "prompt chunk, d 256, blocks of 32": ((1, 1, 256, 32, "bf16", False), 3, [600, 300], [290, 77], (), "layer", (8, 8)),
     "prompt chunk, d 64": ((1, 3, 64, 5, "f16", False), 1, [600, 300], [290, 77], (), "layer", (5, 3)),
     "prompt chunk, fp8": ((2, 2, 128, 16, "fp8_e4m3", True), 2, [500, 91], [200, 30], (), "layer", (0, 0)),
     "prompt chunk, d 192": ((1, 1, 192, 16, "bf16", False), 3, [420, 90], [170, 64], (), "layer", (0, 0)),
@@ -219,6 +221,60 @@ def test_rows_do_not_feel_tokens_that_they_do_not_see(gpu, dtype, what):
     assert (np.abs(got[:bad] - ref[:bad]) <= tol[:bad]).all()
     assert (np.abs(lse.double().cpu().numpy()[:bad] - rlse[:bad]) <= ltol[:bad]).all()
     assert not np.isfinite(got[bad:]).any()
+
+
+@pytest.mark.parametrize("shape", [(2, 72, 5, 3), (1, 64, 16, 8), (2, 192, 4, 2), (1, 256, 32, 4)])
+@pytest.mark.parametrize("new", [2, 5, 90])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8_e4m3"])
+def test_rows_do_not_feel_tokens_that_they_do_not_see_in_any_kernel(gpu, dtype, new, shape):
+    """The same for few and many new tokens and other shapes, with several such tokens, one of them one that all rows see but the first."""
+    import torch
+    H, D, B, G = shape
+    n = 170
+    bad = sorted({n - 1, n - new + 1, n - new // 2})
+    N = -(-n // B) + 2
+    p = Pool(gpu, W.Geometry(1, H, D, B, dtype, N), seed=6)
+    rows = _tables(p.rng, N, [n], B)
+    p.fill(rows, [n])
+    io_name = "f16" if dtype == "f16" else "bf16"
+    q = torch.from_numpy(p.rng.standard_normal((new, G * H, D))).to(_torch_type(io_name)).to(gpu)
+    ref, tol, _, _, _, _ = R.attention(p.values()[0], rows, [n], [new], q.double().cpu().numpy(), D ** -0.5, io_name, B)
+    nan = {"fp8_e4m3": 0x7F, "bf16": 0x7FC0, "f16": 0x7E00}[dtype]
+    for k, x in enumerate(bad):  # one element of V each, and all of K but for the first
+        p.bits()[0, 1, int(rows[0][x // B]), x % B, :, 7 * k] = nan
+        if k:
+            p.bits()[0, 0, int(rows[0][x // B]), x % B] = nan
+    o, ids = R.csr(rows)
+    out = torch.empty_like(q)
+    kv.kv_check(p.batch.set(o, ids, [n], [new], G * H))
+    kv.kv_check(p.batch.attn(0, q, out, D ** -0.5))
+    got = out.double().cpu().numpy()
+    for j in range(new):
+        seen = [k for k, x in enumerate(bad) if x <= n - new + j]
+        if any(seen[1:]) or (seen and seen[0] > 0):
+            assert np.isnan(got[j]).all(), j
+        elif seen:
+            assert np.isnan(got[j][:, 0]).all() and (np.abs(got[j] - ref[j]) <= tol[j])[:, 1:].all(), j
+        else:
+            assert (np.abs(got[j] - ref[j]) <= tol[j]).all(), j
+
+
+def test_a_negative_scale_and_none(gpu):
+    import torch
+    for lens, q_lens in (([300, 70], [1, 1]), ([300, 70], [80, 1])):
+        p = Pool(gpu, W.Geometry(1, 2, 128, 16, "bf16", 30), seed=8)
+        rows = _tables(p.rng, 30, lens, 16)
+        p.fill(rows, lens)
+        o, ids = R.csr(rows)
+        q = torch.from_numpy(p.rng.standard_normal((sum(q_lens), 8, 128))).bfloat16().to(gpu)
+        kv.kv_check(p.batch.set(o, ids, lens, q_lens, 8))
+        for scale in (-0.1, 0.0, -0.0):
+            out, w = torch.empty_like(q), torch.zeros(2, 2, 300, device=gpu)
+            kv.kv_check(p.batch.attn(0, q, out, scale, weights=w))
+            ref, tol, _, _, rw, wtol = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), scale, "bf16", 16)
+            assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
+            for i, n in enumerate(lens):
+                assert (np.abs(w[i, :, :n].double().cpu().numpy() - rw[i]) <= wtol[i] + 2.0 ** -22 * rw[i]).all()
 
 
 def test_attention_far_into_a_pool(gpu):
