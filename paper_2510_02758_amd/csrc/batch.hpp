@@ -17,7 +17,7 @@
 namespace kvswap {
 
 // One piece of attention work for one KV head: a tile of rows against a run of keys.  Nodes of few rows are tiles of their own (at
-// most kRowTile rows), cut and dealt out to workgroups in even shares of keys; nodes of more rows are cut into big tiles.
+// most kRowTile rows), nodes of more rows are cut into big tiles; either kind is dealt out to workgroups in even shares of keys.
 // Row r of a node is new token tokens[first + r / G] with query head r % G of the group.
 struct AttnItem {
   int32_t table;    // where the row of the table begins that names the blocks of the keys
@@ -56,7 +56,7 @@ class BatchPlan {
   std::vector<TokenPlace> places;                            // per row
   std::vector<int32_t> lists;                                // the nodes' tokens
   std::vector<AttnItem> items;                               // first those of row tiles, workgroup by workgroup, then those of big tiles
-  std::vector<int32_t> wg_items;                             // where each workgroup's items begin, and their end
+  std::vector<int32_t> wg_items, wg_big;                     // where each workgroup's items begin, and their end
   int32_t heads = 1;                                         // heads of a workgroup of row tiles: 1, 2 or 4
   int32_t big_first = 0;                                     // first item of a big tile
   std::vector<int32_t> join_off, join;                       // per token: partial rows of its first query head
@@ -228,21 +228,24 @@ class BatchPlan {
   struct Use {
     int32_t list, tokens, part;  // every row of these tokens has a partial row from here on
   };
-  std::vector<Tile> few_, big_;
+  std::vector<Tile> few_, big_, huge_;
   std::vector<int32_t> seen_;  // nodes with keys, per token
   std::vector<Use> uses_;
 
   void cut(const BatchShape& s) {
     lists.clear();
     items.clear();
-    wg_items.clear();
     few_.clear();
     big_.clear();
+    huge_.clear();
     uses_.clear();
     seen_.assign((size_t)T, 0);
     mixed = big_mixed = false;
     partial_rows = 0;
     read = 0;
+    // Tiles have whole tokens, so that a token's rows are together wherever a tile's keys are cut; where one token has more rows than a
+    // big tile, its tiles are cut alike instead.
+    const int32_t big_tokens = s.big_tile / G;
     for (size_t d = 0; d < nodes_.size(); d++) {
       const Node& node = nodes_[d];
       const int32_t list = (int32_t)lists.size();
@@ -251,22 +254,42 @@ class BatchPlan {
       read += node.to - node.from;
       const int32_t tokens = (int32_t)lists.size() - list;
       const int64_t rows = (int64_t)tokens * G;
-      const int32_t size = rows <= kRowTile ? kRowTile : s.big_tile;
-      for (int64_t r = 0; r < rows; r += size) {
-        Tile t{(int32_t)d, list, tokens, (int32_t)r, (int32_t)std::min<int64_t>(size, rows - r), 0, INT32_MAX};
-        for (int64_t j = r / G; j <= (r + t.rows - 1) / G; j++) {
-          const int32_t limit = std::min(node.to, tok_limit[lists[list + j]]);
+      auto tile = [&](int32_t at, int32_t n, int32_t row0, int32_t tile_rows) {
+        Tile t{(int32_t)d, list + at, n, row0, tile_rows, 0, INT32_MAX};
+        for (int32_t j = row0 / G; j <= (row0 + tile_rows - 1) / G; j++) {
+          const int32_t limit = std::min(node.to, tok_limit[lists[list + at + j]]);
           t.limit = std::max(t.limit, limit);
           t.clear = std::min(t.clear, limit);
         }
-        (size == kRowTile ? few_ : big_).push_back(t);
+        return t;
+      };
+      if (rows <= kRowTile) {
+        few_.push_back(tile(0, tokens, 0, (int32_t)rows));
+      } else if (big_tokens > 0) {
+        for (int32_t at = 0; at < tokens; at += big_tokens) {
+          const int32_t n = std::min(big_tokens, tokens - at);
+          big_.push_back(tile(at, n, 0, n * G));
+        }
+      } else {
+        for (int64_t r = 0; r < rows; r += s.big_tile)
+          huge_.push_back(tile(0, tokens, (int32_t)r, (int32_t)std::min<int64_t>(s.big_tile, rows - r)));
       }
       for (size_t j = list; j < lists.size(); j++)
         if (node.to > node.from) seen_[lists[j]]++;
     }
-    deal_out(s);
+    heads = 1;
+    int64_t work = 0;
+    for (const Tile& t : few_) work += std::max(t.limit - nodes_[t.node].from, 0);
+    // Where there is enough for every workgroup, its four wavefronts take four heads (two, if the head count is no multiple of four) rather
+    // than four runs of one head's keys: they then read neighbouring bytes at the same time.  64 requests of 512 to 4096 tokens with 8
+    // heads of 128 in bf16: 106 us instead of 134, 32 requests of 256 to 8192 with 32 heads in fp8: 188 instead of 209.
+    heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
+    wg_items.clear();
+    deal_out(few_, s.wgs * heads / s.H, s.least / heads, s.B, &wg_items, &mixed);
     big_first = (int32_t)items.size();
-    cut_big(s);
+    wg_big.clear();
+    deal_out(big_, s.big_wgs / s.H, s.big_least, s.B, &wg_big, &big_mixed);
+    cut_alike(s.B);
 
     join_off.assign((size_t)T + 1, 0);
     for (const Use& u : uses_)
@@ -301,39 +324,47 @@ class BatchPlan {
     items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part});
     if (items.back().clear < end) *any_mixed = true;
   }
+  int32_t take_rows(const Tile& t, int32_t rows) {
+    const int32_t part = partial_rows;
+    partial_rows += rows;
+    uses_.push_back({t.list, t.tokens, part});
+    return part;
+  }
 
-  // Row tiles.  If one piece of at most `share` keys for each workgroup that the device holds is enough, every tile is cut by itself, and
-  // each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares: a workgroup may take the end
-  // of one tile, whole ones and the beginning of another.
-  void deal_out(const BatchShape& s) {
+  // Tiles of whole tokens.  If one piece of at most `share` keys for each of the workgroups that are to run at a time (`held`) is enough, every tile is cut by
+  // itself, and each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares: a workgroup may take
+  // the end of one tile, whole ones and the beginning of another.
+  void deal_out(const std::vector<Tile>& tiles, int64_t held, int64_t least, int32_t B, std::vector<int32_t>* wgs, bool* any_mixed) {
     int64_t work = 0;
-    for (const Tile& t : few_) work += std::max(t.limit - nodes_[t.node].from, 0);
-    // Where there is enough for every workgroup, its four wavefronts take four heads (two, if the head count is no multiple of four) rather
-    // than four runs of one head's keys: they then read neighbouring bytes at the same time.  64 requests of 512 to 4096 tokens with 8
-    // heads of 128 in bf16: 106 us instead of 134, 32 requests of 256 to 8192 with 32 heads in fp8: 188 instead of 209.
-    heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
-    const int64_t held = std::max<int64_t>(1, s.wgs * heads / s.H), most = most_keys(s.B);
-    int64_t share = std::max<int64_t>(s.least / heads, (work + held - 1) / held);
+    for (const Tile& t : tiles) work += std::max(t.limit - nodes_[t.node].from, 0);
+    held = std::max<int64_t>(1, held);
+    const int64_t most = most_keys(B);
+    int64_t share = std::max<int64_t>(least, (work + held - 1) / held);
     share = std::min(most, (share + kStep - 1) / kStep * kStep);
+    // Tiles that all have a workgroup of their own stay whole if the longest is not much longer than a share: partial results cost more
+    // (two prompts' chunks of 1024 and 517 tokens behind 8001 and 5000: 207 us whole, 219 in equal shares).
+    int64_t longest = 0;
+    for (const Tile& t : tiles) longest = std::max<int64_t>(longest, t.limit - nodes_[t.node].from);
+    if ((int64_t)tiles.size() <= held && longest <= share + share * 5 / 8 && longest <= most) share = std::max(share, longest);
     int64_t pieces = 0;
-    for (const Tile& t : few_) pieces += std::max<int64_t>(1, (std::max(t.limit - nodes_[t.node].from, 0) + share - 1) / share);
+    for (const Tile& t : tiles) pieces += std::max<int64_t>(1, (std::max(t.limit - nodes_[t.node].from, 0) + share - 1) / share);
     const bool line = pieces > held;
     int64_t room = 0;  // keys that the current workgroup still takes
-    for (const Tile& t : few_) {
+    for (const Tile& t : tiles) {
       if (idle(t)) continue;
       const int32_t from = nodes_[t.node].from, keys = std::max(t.limit - from, 0);
       const bool whole_alone = alone(t);
       if (!line || keys == 0 || room < kStep) {
-        wg_items.push_back((int32_t)items.size());
+        wgs->push_back((int32_t)items.size());
         room = share;
       }
       if (!line) {  // equal pieces
         const int32_t n = (int32_t)std::max<int64_t>(1, (keys + share - 1) / share);
         const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + kStep - 1) / kStep * kStep);
         for (int32_t c = 0; c < n && (c == 0 || (int64_t)c * step < keys); c++) {
-          if (c) wg_items.push_back((int32_t)items.size());
-          const int32_t part = n == 1 && whole_alone ? -1 : take_rows(t);
-          add(t, from + c * step, from + (int32_t)std::min<int64_t>(keys, (int64_t)(c + 1) * step), part, &mixed);
+          if (c) wgs->push_back((int32_t)items.size());
+          const int32_t part = n == 1 && whole_alone ? -1 : take_rows(t, t.rows);
+          add(t, from + c * step, from + (int32_t)std::min<int64_t>(keys, (int64_t)(c + 1) * step), part, any_mixed);
         }
         continue;
       }
@@ -341,54 +372,36 @@ class BatchPlan {
       for (int32_t k = 0; k < keys || keys == 0;) {
         int32_t n = (int32_t)std::min<int64_t>(keys - k, room);
         if (keys - k - n < kStep / 2 && keys - k <= most) n = keys - k;
-        const int32_t part = n == keys && whole_alone ? -1 : take_rows(t);
-        add(t, from + k, from + k + n, part, &mixed);
+        const int32_t part = n == keys && whole_alone ? -1 : take_rows(t, t.rows);
+        add(t, from + k, from + k + n, part, any_mixed);
         k += n;
         room -= (n + kStep - 1) / kStep * kStep;
         if (keys == 0) break;
         if (k < keys) {
-          wg_items.push_back((int32_t)items.size());
+          wgs->push_back((int32_t)items.size());
           room = share;
         }
       }
     }
-    wg_items.push_back((int32_t)items.size());
-  }
-  int32_t take_rows(const Tile& t) {
-    const int32_t part = partial_rows;
-    partial_rows += t.rows;  // a row tile has all rows of its tokens
-    uses_.push_back({t.list, t.tokens, part});
-    return part;
+    wgs->push_back((int32_t)items.size());
   }
 
-  // Big tiles: all tiles of a node are cut at the same keys, into equal pieces, so many that the device is full.
-  void cut_big(const BatchShape& s) {
-    int64_t work = 0;
-    for (const Tile& t : big_) work += std::max(t.limit - nodes_[t.node].from, 0);
-    int64_t chunk = (work * s.H + s.big_wgs - 1) / s.big_wgs;
-    chunk = std::min(most_keys(s.B), std::max<int64_t>(s.big_least, (chunk + kStep - 1) / kStep * kStep));
-    for (size_t k = 0; k < big_.size();) {
+  // Tiles that share tokens: all of a node's are cut at the same keys, as seldom as may be.  They follow the big tiles.
+  void cut_alike(int32_t B) {
+    const int64_t most = most_keys(B);
+    for (size_t k = 0; k < huge_.size();) {
       size_t e = k;
-      while (e < big_.size() && big_[e].node == big_[k].node) e++;
-      const Node& node = nodes_[big_[k].node];
-      if (idle(big_[k])) {
-        k = e;
-        continue;
-      }
-      const int32_t keys = node.to - node.from, n = (int32_t)std::max<int64_t>(1, (keys + chunk - 1) / chunk);
-      const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + kStep - 1) / kStep * kStep);
-      const bool direct = n == 1 && alone(big_[k]);
-      for (int32_t c = 0; c < n && (c == 0 || (int64_t)c * step < keys); c++) {
-        int32_t part = -1;
-        if (!direct) {
-          part = partial_rows;
-          partial_rows += big_[k].tokens * G;
-          uses_.push_back({big_[k].list, big_[k].tokens, part});
+      while (e < huge_.size() && huge_[e].node == huge_[k].node) e++;
+      const Node& node = nodes_[huge_[k].node];
+      const int64_t keys = node.to - node.from;
+      if (!idle(huge_[k]))
+        for (int64_t c = 0; c == 0 || c < keys; c += most) {
+          const int32_t part = keys <= most && alone(huge_[k]) ? -1 : take_rows(huge_[k], huge_[k].tokens * G);
+          for (size_t j = k; j < e; j++) {
+            add(huge_[j], node.from + (int32_t)c, node.from + (int32_t)std::min(keys, c + most), part < 0 ? -1 : part + huge_[j].row0, &big_mixed);
+            wg_big.push_back((int32_t)items.size());
+          }
         }
-        for (size_t j = k; j < e; j++)
-          add(big_[j], node.from + c * step, node.from + (int32_t)std::min<int64_t>(keys, (int64_t)(c + 1) * step), direct ? -1 : part + big_[j].row0,
-              &big_mixed);
-      }
       k = e;
     }
   }

@@ -37,7 +37,7 @@ struct kv_batch {
   hipEvent_t up_ev[2] = {nullptr, nullptr};
   bool up_busy[2] = {false, false};
   int turn = 0;
-  const int32_t *wg_items = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
+  const int32_t *wg_items = nullptr, *wg_big = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
                 *join_off = nullptr, *join = nullptr;
   const AttnItem* items = nullptr;
   const WeightItem* witems = nullptr;
@@ -162,37 +162,37 @@ constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }
 template <typename E, bool P, int DP>
 struct LaunchAttn {
   static void go(const AttnArgs* a, const BatchPlan* pl, hipStream_t st) {
-    constexpr int N = DP / 16;
-    constexpr size_t table = BatchPlan::kMaxEntries * 4, join = 2 * 64 * 4 * N * 4 + 2 * 16 * 8, keys = 4 * 32 * DP * (P ? 1 : 2);
-    const int wgs = ((int)pl->wg_items.size() - 1) * (a->H / a->hw), big = ((int)pl->items.size() - pl->big_first) * a->H;
-    auto launch = [&](auto kern, int n, const AttnArgs& args, size_t lds) { hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, st, args); };
-    if (wgs) {
-      if (pl->mixed)
-        launch(kv_attn_kernel<E, P, DP, true>, wgs, *a, std::max(table, join));
-      else if (a->kv.D == DP && a->kv.B % 16 == 0)
-        launch(kv_attn_stream_kernel<E, P, DP>, wgs, *a, std::max(keys + table, join));
+    constexpr int N = DP / 16, C = big_tile(DP) / 64;
+    constexpr size_t table = BatchPlan::kMaxEntries * 4, join = 2 * 64 * 4 * N * 4 + 2 * 16 * 8;
+    constexpr size_t row_lds = std::max(table, join), stream_lds = std::max(4 * 32 * DP * (P ? 1 : 2) + table, join);
+    constexpr size_t tile_lds = 4 * 2 * (DP / 32) * 1024 + 4 * N * 1024 + (P ? 4 * 2 * 32 * 4 : 0) + 16 + table, big_lds = 4 * 64 * DP * 2 + 16 + table;
+    const int rows = ((int)pl->wg_items.size() - 1) * (a->H / a->hw), bigs = ((int)pl->wg_big.size() - 1) * a->H;
+    const bool fast = a->kv.D == DP && a->kv.B % 16 == 0, stream = fast && !pl->mixed;
+    auto launch = [&](auto kern, int n, size_t lds, auto... more) { hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, st, *a, more...); };
+    if (rows && bigs && stream) {
+      constexpr size_t lds = std::max(stream_lds, P ? tile_lds : big_lds);
+      if (pl->big_mixed)
+        launch(kv_attn_both_kernel<E, P, DP, C, true>, rows + bigs, lds, rows, bigs);
       else
-        launch(kv_attn_kernel<E, P, DP, false>, wgs, *a, std::max(table, join));
+        launch(kv_attn_both_kernel<E, P, DP, C, false>, rows + bigs, lds, rows, bigs);
+      return;
     }
-    if (big) {
-      constexpr int C = big_tile(DP) / 64;
-      constexpr size_t lds = 4 * 2 * (DP / 32) * 1024 + 4 * N * 1024 + (P ? 4 * 2 * 32 * 4 : 0) + 16 + table;
-      AttnArgs b = *a;
-      b.items += pl->big_first;
+    if (rows) {
+      if (stream)
+        launch(kv_attn_stream_kernel<E, P, DP>, rows, stream_lds);
+      else if (pl->mixed)
+        launch(kv_attn_kernel<E, P, DP, true>, rows, row_lds);
+      else
+        launch(kv_attn_kernel<E, P, DP, false>, rows, row_lds);
+    }
+    if (bigs) {
       if constexpr (!P) {
-        if (a->kv.D == DP && a->kv.B % 16 == 0) {
-          constexpr size_t own = 4 * 64 * DP * 2 + 16 + table;
-          if (pl->big_mixed)
-            launch(kv_attn_big_kernel<E, DP, C, true>, big, b, own);
-          else
-            launch(kv_attn_big_kernel<E, DP, C, false>, big, b, own);
+        if (fast) {
+          pl->big_mixed ? launch(kv_attn_big_kernel<E, P, DP, C, true, true>, bigs, big_lds) : launch(kv_attn_big_kernel<E, P, DP, C, false, true>, bigs, big_lds);
           return;
         }
       }
-      if (pl->big_mixed)
-        launch(kv_attn_tile_kernel<E, P, DP, C, true>, big, b, lds);
-      else
-        launch(kv_attn_tile_kernel<E, P, DP, C, false>, big, b, lds);
+      pl->big_mixed ? launch(kv_attn_big_kernel<E, P, DP, C, true, false>, bigs, tile_lds) : launch(kv_attn_big_kernel<E, P, DP, C, false, false>, bigs, tile_lds);
     }
   }
 };
@@ -286,7 +286,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     const void** at;
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
-  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
+  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
                         VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
                         VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
 #undef VEC
@@ -478,6 +478,7 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   k.kv = side(b, a->layer);
   k.items = b->items;
   k.wg_items = b->wg_items;
+  k.wg_big = b->wg_big;
   k.lists = b->lists;
   k.limit = b->limit;
   k.table = b->table;
@@ -510,9 +511,9 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
     const dim3 grid((unsigned)pl.T * v.H * pl.G);
     auto go = [&](auto e) {
       using E = decltype(e);
-      if (pl.most_parts <= 8)
+      if (pl.most_parts <= 32)
         hipLaunchKernelGGL((kv_attn_join_kernel<E, 1>), grid, dim3(64), 0, st, j);
-      else if (pl.most_parts <= 32)
+      else if (pl.most_parts <= 96)
         hipLaunchKernelGGL((kv_attn_join_kernel<E, 4>), grid, dim3(256), 0, st, j);
       else
         hipLaunchKernelGGL((kv_attn_join_kernel<E, 16>), grid, dim3(1024), 0, st, j);

@@ -21,7 +21,7 @@
 
 int main(int argc, char** argv) {
   const int seeds = argc > 1 ? atoi(argv[1]) : 400;
-  long shared_nodes = 0, joined = 0, direct = 0, dealt = 0;
+  long shared_nodes = 0, joined = 0, direct = 0, dealt = 0, big_dealt = 0;
   for (int seed = 0; seed < seeds; seed++) {
     std::mt19937 rng(seed);
     auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
@@ -29,7 +29,7 @@ int main(int argc, char** argv) {
     const int Bs[] = {1, 3, 4, 16, 20, 32};
     s.B = Bs[pick(0, 5)];
     s.H = pick(1, 4);
-    const int G = pick(1, 20);
+    const int G = pick(0, 9) ? pick(1, 20) : pick(60, 150);
     s.N = 1 << 20;
     s.wgs = pick(0, 1) ? 1024 : pick(1, 64);
     s.big_tile = pick(0, 1) ? 128 : 64;
@@ -112,6 +112,11 @@ int main(int argc, char** argv) {
     // every row tile's item has its workgroup
     CHECK(p.wg_items.size() >= 1 && p.wg_items.back() == p.big_first, "workgroups");
     for (size_t k = 0; k + 1 < p.wg_items.size(); k++) CHECK(p.wg_items[k] < p.wg_items[k + 1] && (k || p.wg_items[0] == 0), "workgroup %zu", k);
+    CHECK(p.wg_big.size() >= 1 && p.wg_big[0] == p.big_first && p.wg_big.back() == (int)p.items.size(), "workgroups of big tiles");
+    for (size_t k = 0; k + 1 < p.wg_big.size(); k++) {
+      CHECK(p.wg_big[k] < p.wg_big[k + 1], "workgroup %zu of big tiles", k);
+      big_dealt += p.wg_big[k + 1] - p.wg_big[k] > 1;
+    }
     for (size_t k = 0; k + 1 < p.wg_items.size(); k++) dealt += p.wg_items[k + 1] - p.wg_items[k] > 1;
     int64_t cached = 0;
     for (int i = 0; i < n; i++)
@@ -129,8 +134,8 @@ int main(int argc, char** argv) {
       for (auto& k : w[i]) CHECK(k.second == 1 && k.first < len[i], "weight of key %d", k.first);
     }
   }
-  if (!shared_nodes || !joined || !direct || !dealt) {
-    fprintf(stderr, "the batches do not reach every kind: %ld shared, %ld joined, %ld direct, %ld dealt\n", shared_nodes, joined, direct, dealt);
+  if (!shared_nodes || !joined || !direct || !dealt || !big_dealt) {
+    fprintf(stderr, "the batches do not reach every kind: %ld shared, %ld joined, %ld direct, %ld and %ld dealt\n", shared_nodes, joined, direct, dealt, big_dealt);
     return 1;
   }
   printf("plans ok: %ld batches with shared keys, %ld rows joined, %ld finished at once\n", shared_nodes, joined, direct);
