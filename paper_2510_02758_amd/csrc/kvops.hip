@@ -8,12 +8,10 @@
 #include <mutex>
 #include <new>
 #include <stdexcept>
-#include <type_traits>
 
 #include "pool_view.hpp"
-#include "batch.hpp"
+#include "attn.hpp"
 
-#include "attn.hip.inc"
 #include "append.hip.inc"
 #include "evict.hip.inc"
 
@@ -135,73 +133,6 @@ bool aligned(const void* p, const int64_t* strides, int bytes) {
   const int el = bytes / 2;
   return (uintptr_t)p % bytes == 0 && strides[0] % el == 0 && strides[1] % el == 0;
 }
-
-// f<element type of the products, pool of fp8, padded head size>
-template <template <typename, bool, int> class F, typename... A>
-void by_type(const PoolView& v, int32_t io, A... args) {
-  const bool fp8 = v.dtype == KV_FP8_E4M3;
-  auto by_size = [&](auto e, auto f) {
-    using E = decltype(e);
-    constexpr bool P = decltype(f)::value;
-    if (v.D <= 64)
-      F<E, P, 64>::go(args...);
-    else if (v.D <= 128)
-      F<E, P, 128>::go(args...);
-    else
-      F<E, P, 256>::go(args...);
-  };
-  if (io == KV_F16)
-    fp8 ? by_size(_Float16(), std::true_type()) : by_size(_Float16(), std::false_type());
-  else
-    fp8 ? by_size(__bf16(), std::true_type()) : by_size(__bf16(), std::false_type());
-}
-
-// Rows of a big tile: what a wavefront's registers hold of their outputs.
-constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }
-
-template <typename E, bool P, int DP>
-struct LaunchAttn {
-  static void go(const AttnArgs* a, const BatchPlan* pl, hipStream_t st) {
-    constexpr int N = DP / 16, C = big_tile(DP) / 64;
-    constexpr size_t table = BatchPlan::kMaxEntries * 4, join = 2 * 64 * 4 * N * 4 + 2 * 16 * 8;
-    constexpr size_t row_lds = std::max(table, join), stream_lds = std::max(4 * 32 * DP * (P ? 1 : 2) + table, join);
-    constexpr size_t tile_lds = 4 * 2 * (DP / 32) * 1024 + 4 * N * 1024 + (P ? 4 * 2 * 32 * 4 : 0) + 16 + table, big_lds = 4 * 64 * DP * 2 + 16 + table;
-    const int rows = ((int)pl->wg_items.size() - 1) * (a->H / a->hw), bigs = ((int)pl->wg_big.size() - 1) * a->H;
-    const bool fast = a->kv.D == DP && a->kv.B % 16 == 0, stream = fast && !pl->mixed;
-    auto launch = [&](auto kern, int n, size_t lds, auto... more) { hipLaunchKernelGGL(kern, dim3(n), dim3(256), lds, st, *a, more...); };
-    if (rows && bigs && stream) {
-      constexpr size_t lds = std::max(stream_lds, P ? tile_lds : big_lds);
-      if (pl->big_mixed)
-        launch(kv_attn_both_kernel<E, P, DP, C, true>, rows + bigs, lds, rows, bigs);
-      else
-        launch(kv_attn_both_kernel<E, P, DP, C, false>, rows + bigs, lds, rows, bigs);
-      return;
-    }
-    if (rows) {
-      if (stream)
-        launch(kv_attn_stream_kernel<E, P, DP>, rows, stream_lds);
-      else if (pl->mixed)
-        launch(kv_attn_kernel<E, P, DP, true>, rows, row_lds);
-      else
-        launch(kv_attn_kernel<E, P, DP, false>, rows, row_lds);
-    }
-    if (bigs) {
-      if constexpr (!P) {
-        if (fast) {
-          pl->big_mixed ? launch(kv_attn_big_kernel<E, P, DP, C, true, true>, bigs, big_lds) : launch(kv_attn_big_kernel<E, P, DP, C, false, true>, bigs, big_lds);
-          return;
-        }
-      }
-      pl->big_mixed ? launch(kv_attn_big_kernel<E, P, DP, C, true, false>, bigs, tile_lds) : launch(kv_attn_big_kernel<E, P, DP, C, false, false>, bigs, tile_lds);
-    }
-  }
-};
-template <typename E, bool P, int DP>
-struct LaunchWeights {
-  static void go(const WeightArgs* w, int items, hipStream_t st) {
-    hipLaunchKernelGGL((kv_attn_weights_kernel<E, P, DP>), dim3(items * w->a.H), dim3(256), BatchPlan::kMaxEntries * 4, st, *w);
-  }
-};
 
 }  // namespace
 
@@ -504,26 +435,17 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   k.hw = pl.heads;
   k.q_vec = aligned(a->q, a->q_strides, 16);
   k.o_vec = aligned(a->out, a->out_strides, 8);
-  by_type<LaunchAttn>(v, a->io_dtype, (const AttnArgs*)&k, &pl, st);
+  const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16;
+  f16 ? launch_attn<_Float16>(fp8, k, pl, st) : launch_attn<__bf16>(fp8, k, pl, st);
   OPCHK(b, hipGetLastError());
   if (pl.partial_rows) {
     JoinArgs j{b->join_off, b->join, b->part_o, b->part_ml, k.out, k.o_ts, k.o_hs, k.lse, k.lse_ts, v.H, pl.G, v.D};
-    const dim3 grid((unsigned)pl.T * v.H * pl.G);
-    auto go = [&](auto e) {
-      using E = decltype(e);
-      if (pl.most_parts <= 32)
-        hipLaunchKernelGGL((kv_attn_join_kernel<E, 1>), grid, dim3(64), 0, st, j);
-      else if (pl.most_parts <= 96)
-        hipLaunchKernelGGL((kv_attn_join_kernel<E, 4>), grid, dim3(256), 0, st, j);
-      else
-        hipLaunchKernelGGL((kv_attn_join_kernel<E, 16>), grid, dim3(1024), 0, st, j);
-    };
-    a->io_dtype == KV_F16 ? go(_Float16()) : go(__bf16());
+    f16 ? launch_join<_Float16>(j, pl, st) : launch_join<__bf16>(j, pl, st);
     OPCHK(b, hipGetLastError());
   }
   if (a->weights && !pl.witems.empty()) {
     WeightArgs w{k, b->witems, b->q_first, b->off, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
-    by_type<LaunchWeights>(v, a->io_dtype, (const WeightArgs*)&w, (int)pl.witems.size(), st);
+    f16 ? launch_weights<_Float16>(fp8, w, pl, st) : launch_weights<__bf16>(fp8, w, pl, st);
     OPCHK(b, hipGetLastError());
   }
   return KV_OK;
