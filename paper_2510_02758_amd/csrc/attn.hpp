@@ -44,6 +44,8 @@ struct AttnArgs {
   int32_t flip;  // the scale is negative: queries change sign
   int32_t H, G, q_vec;
   int32_t o_vec;
+  float* scores;         // null: the products of row tiles are not kept
+  int64_t scores_head;   // of one KV head
   int32_t hw;  // heads of a workgroup of row tiles (1, 2 or 4): its wavefronts take one each, and 4 / hw share a head's keys
 };
 
@@ -75,13 +77,26 @@ struct WeightArgs {
   int64_t w_rs, w_hs;
 };
 
+struct SumArgs {
+  const kvswap::ScoreItem* items;
+  const int32_t* q_first;
+  const float* scores;
+  int64_t scores_head;
+  const float* lse;
+  int64_t lse_ts;
+  float* weights;
+  int64_t w_rs, w_hs;
+  float scale2;
+  int32_t H, G;
+};
+
 // Enqueue the batch's tiles, the join of its partial results, its weight items.  E: the type of the products.
 template <typename E>
 void launch_attn(bool fp8, const AttnArgs& a, const kvswap::BatchPlan& pl, hipStream_t st);
 template <typename E>
 void launch_join(const JoinArgs& j, const kvswap::BatchPlan& pl, hipStream_t st);
 template <typename E>
-void launch_weights(bool fp8, const WeightArgs& w, const kvswap::BatchPlan& pl, hipStream_t st);
+void launch_weights(bool fp8, const WeightArgs& w, int items, hipStream_t st);
 
 // Rows of a big tile: what a wavefront's registers hold of their outputs.
 constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }

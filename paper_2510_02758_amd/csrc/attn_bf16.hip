@@ -8,4 +8,4 @@
 
 template void launch_attn<__bf16>(bool, const AttnArgs&, const kvswap::BatchPlan&, hipStream_t);
 template void launch_join<__bf16>(const JoinArgs&, const kvswap::BatchPlan&, hipStream_t);
-template void launch_weights<__bf16>(bool, const WeightArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_weights<__bf16>(bool, const WeightArgs&, int, hipStream_t);

@@ -8,4 +8,4 @@
 
 template void launch_attn<_Float16>(bool, const AttnArgs&, const kvswap::BatchPlan&, hipStream_t);
 template void launch_join<_Float16>(const JoinArgs&, const kvswap::BatchPlan&, hipStream_t);
-template void launch_weights<_Float16>(bool, const WeightArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_weights<_Float16>(bool, const WeightArgs&, int, hipStream_t);

@@ -26,10 +26,16 @@ struct AttnItem {
   int32_t tokens;   // the node's list of tokens
   int32_t row0, rows;
   int32_t part;     // partial row of row0; -1: the rows are finished here
+  // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
+  int32_t score, score_row, score_from, pad;
 };
-// One piece of weight accumulation: keys [k0, k1) of a request.
+// One piece of weight accumulation: keys [k0, k1) of a request, whose products are computed again.
 struct WeightItem {
   int32_t req, k0, k1, pad;
+};
+// The same from products that were kept: the request's rows are row0 .. row0+rows-1 of their tile.
+struct ScoreItem {
+  int32_t req, k0, k1, score, score_row, score_from, row0, rows;
 };
 
 // Where a new token goes: place `place` of block `block` (-1: nowhere), cache index `index`.
@@ -60,14 +66,17 @@ class BatchPlan {
   int32_t heads = 1;                                         // heads of a workgroup of row tiles: 1, 2 or 4
   int32_t big_first = 0;                                     // first item of a big tile
   std::vector<int32_t> join_off, join;                       // per token: partial rows of its first query head
-  std::vector<WeightItem> witems;
+  // Weights: of all keys from products computed again; or of row tiles' keys from kept ones, and of the others computed again.
+  std::vector<WeightItem> witems, wrest;
+  std::vector<ScoreItem> sitems;
+  int64_t scores = 0;                                        // kept products of one KV head
   int32_t partial_rows = 0, most_parts = 0;
   bool mixed = false, big_mixed = false;  // some row tile (big tile) has keys that some of its rows see and others do not
 
   // Entries of the table that an item may need: its part of the table is held on chip.
   static constexpr int32_t kMaxEntries = 2048;
   static constexpr int32_t kRowTile = 16;
-  static constexpr int32_t kWeightKeys = 512;
+  static constexpr int32_t kWeightKeys = 512, kScoreKeys = 1024;
 
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
           const BatchShape& s) {
@@ -84,7 +93,7 @@ class BatchPlan {
       table += need;
     }
     const int32_t g = num_q_heads / s.H;
-    if (rows * g > INT32_MAX / 4 || table > INT32_MAX) return KV_EINVAL;
+    if (rows * g > INT32_MAX / 4 || table > INT32_MAX || (keys + 16 * (int64_t)n_) * kRowTile / 16 > INT32_MAX) return KV_EINVAL;
     if (table && !blocks) return KV_EINVAL;
     for (int32_t i = 0; i < n_; i++) {
       const int64_t need = ((int64_t)tokens[i] + s.B - 1) / s.B;
@@ -224,6 +233,7 @@ class BatchPlan {
 
   struct Tile {
     int32_t node, list, tokens, row0, rows, limit, clear;
+    int32_t score = 0, score_row = 0;
   };
   struct Use {
     int32_t list, tokens, part;  // every row of these tokens has a partial row from here on
@@ -239,6 +249,9 @@ class BatchPlan {
     big_.clear();
     huge_.clear();
     uses_.clear();
+    wrest.clear();
+    sitems.clear();
+    scores = 0;
     seen_.assign((size_t)T, 0);
     mixed = big_mixed = false;
     partial_rows = 0;
@@ -264,7 +277,17 @@ class BatchPlan {
         return t;
       };
       if (rows <= kRowTile) {
-        few_.push_back(tile(0, tokens, 0, (int32_t)rows));
+        Tile t = tile(0, tokens, 0, (int32_t)rows);
+        t.score_row = (std::max(t.limit - node.from, 0) + 15) / 16 * 16;
+        t.score = (int32_t)(scores / 16);
+        scores += (int64_t)rows * t.score_row;
+        int32_t row0 = 0;
+        for (int32_t i : node.reqs) {
+          for (int32_t k = node.from; k < t.limit; k += kScoreKeys)
+            sitems.push_back({i, k, std::min(t.limit, k + kScoreKeys), t.score, t.score_row, node.from, row0, q_len[i] * G});
+          row0 += q_len[i] * G;
+        }
+        few_.push_back(t);
       } else if (big_tokens > 0) {
         for (int32_t at = 0; at < tokens; at += big_tokens) {
           const int32_t n = std::min(big_tokens, tokens - at);
@@ -274,6 +297,9 @@ class BatchPlan {
         for (int64_t r = 0; r < rows; r += s.big_tile)
           huge_.push_back(tile(0, tokens, (int32_t)r, (int32_t)std::min<int64_t>(s.big_tile, rows - r)));
       }
+      if (rows > kRowTile)
+        for (int32_t i : node.reqs)
+          for (int32_t k = node.from; k < node.to; k += kWeightKeys) wrest.push_back({i, k, std::min(node.to, k + kWeightKeys), 0});
       for (size_t j = list; j < lists.size(); j++)
         if (node.to > node.from) seen_[lists[j]]++;
     }
@@ -321,7 +347,8 @@ class BatchPlan {
 
   void add(const Tile& t, int32_t k0, int32_t k1, int32_t part, bool* any_mixed) {
     const int32_t end = std::max(k0, std::min(k1, t.limit));
-    items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part});
+    items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part,
+                     t.score, t.score_row, nodes_[t.node].from, 0});
     if (items.back().clear < end) *any_mixed = true;
   }
   int32_t take_rows(const Tile& t, int32_t rows) {

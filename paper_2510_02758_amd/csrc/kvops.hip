@@ -12,12 +12,14 @@
 #include "pool_view.hpp"
 #include "attn.hpp"
 
+#include "attn_sum.hip.inc"
 #include "append.hip.inc"
 #include "evict.hip.inc"
 
 using kvswap::AttnItem;
 using kvswap::BatchPlan;
 using kvswap::PoolView;
+using kvswap::ScoreItem;
 using kvswap::TokenPlace;
 using kvswap::WeightItem;
 
@@ -38,7 +40,8 @@ struct kv_batch {
   const int32_t *wg_items = nullptr, *wg_big = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
                 *join_off = nullptr, *join = nullptr;
   const AttnItem* items = nullptr;
-  const WeightItem* witems = nullptr;
+  const WeightItem *witems = nullptr, *wrest = nullptr;
+  const ScoreItem* sitems = nullptr;
   const TokenPlace* places = nullptr;
 
   // Partial results and, for callers that want weights without lse, the lse.
@@ -46,6 +49,10 @@ struct kv_batch {
   size_t ws_cap = 0;
   float *part_o = nullptr, *lse = nullptr;
   float2* part_ml = nullptr;
+
+  // Products of row tiles that the weights are computed from, taken when weights are first asked for (and not in a capture).
+  float* scores = nullptr;
+  size_t scores_cap = 0;
 
   // The stream of the newest work; another stream's call waits for what is on it.
   bool used = false;
@@ -80,6 +87,25 @@ int caught() noexcept {
 bool is_capturing(hipStream_t st) {
   hipStreamCaptureStatus s = hipStreamCaptureStatusNone;
   return hipStreamIsCapturing(st, &s) != hipSuccess || s != hipStreamCaptureStatusNone;
+}
+
+// Room for the batch's kept products; false: there is none, they have to be computed again.
+bool scores_room(kv_batch* b, hipStream_t st) {
+  const size_t need = (size_t)b->plan.scores * b->v.H * 4;
+  if (need <= b->scores_cap) return true;
+  if (is_capturing(st)) return false;
+  if (b->scores) {  // earlier calls may still use it; hipFree waits for them
+    (void)hipFree(b->scores);
+    b->scores = nullptr;
+    b->scores_cap = 0;
+  }
+  if (hipMalloc((void**)&b->scores, need + need / 4) != hipSuccess) {
+    (void)hipGetLastError();
+    b->scores = nullptr;
+    return false;
+  }
+  b->scores_cap = need + need / 4;
+  return true;
 }
 
 // Puts `st` behind the batch's work on another stream.
@@ -178,6 +204,7 @@ int kv_batch_destroy(kv_batch* b) try {
       if (u) (void)hipHostFree(u);
     if (b->mem) (void)hipFree(b->mem);
     if (b->ws) (void)hipFree(b->ws);
+    if (b->scores) (void)hipFree(b->scores);
   }
   delete b;
   return rc;
@@ -217,7 +244,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     const void** at;
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
-  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
+  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems), VEC(pl.wrest, b->wrest), VEC(pl.sitems, b->sitems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
                         VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
                         VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
 #undef VEC
@@ -435,6 +462,11 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   k.hw = pl.heads;
   k.q_vec = aligned(a->q, a->q_strides, 16);
   k.o_vec = aligned(a->out, a->out_strides, 8);
+  const bool keeps = a->weights && pl.scores && scores_room(b, st);
+  if (keeps) {
+    k.scores = b->scores;
+    k.scores_head = pl.scores;
+  }
   const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16;
   f16 ? launch_attn<_Float16>(fp8, k, pl, st) : launch_attn<__bf16>(fp8, k, pl, st);
   OPCHK(b, hipGetLastError());
@@ -443,9 +475,15 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
     f16 ? launch_join<_Float16>(j, pl, st) : launch_join<__bf16>(j, pl, st);
     OPCHK(b, hipGetLastError());
   }
-  if (a->weights && !pl.witems.empty()) {
-    WeightArgs w{k, b->witems, b->q_first, b->off, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
-    f16 ? launch_weights<_Float16>(fp8, w, pl, st) : launch_weights<__bf16>(fp8, w, pl, st);
+  if (a->weights && keeps) {
+    const SumArgs s{b->sitems, b->q_first, k.scores, k.scores_head, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1], k.scale2, v.H, pl.G};
+    hipLaunchKernelGGL(kv_attn_sum_kernel, dim3((unsigned)pl.sitems.size() * v.H), dim3(256), 0, st, s);
+    OPCHK(b, hipGetLastError());
+  }
+  const std::vector<WeightItem>& again = keeps ? pl.wrest : pl.witems;
+  if (a->weights && !again.empty()) {
+    WeightArgs w{k, keeps ? b->wrest : b->witems, b->q_first, b->off, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
+    f16 ? launch_weights<_Float16>(fp8, w, (int)again.size(), st) : launch_weights<__bf16>(fp8, w, (int)again.size(), st);
     OPCHK(b, hipGetLastError());
   }
   return KV_OK;

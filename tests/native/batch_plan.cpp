@@ -123,6 +123,35 @@ int main(int argc, char** argv) {
       if (ql[i]) cached += len[i];
     CHECK(p.read <= cached, "reads %lld of %lld", (long long)p.read, (long long)cached);
     shared_nodes += p.read < cached;
+    // kept products: every (row, key) of a row tile has a place of its own, and each request's keys are summed once, from
+    // kept products by the places that its rows wrote, or computed again
+    std::map<int64_t, std::pair<int, int>> place;  // -> (row, key)
+    for (int n2 = 0; n2 < p.big_first; n2++) {
+      const auto& it = p.items[n2];
+      for (int r = 0; r < it.rows; r++)
+        for (int x = it.k0; x < it.k1; x++) {
+          const int64_t at = (int64_t)it.score * 16 + (int64_t)r * it.score_row + x - it.score_from;
+          CHECK(at >= 0 && at < p.scores && !place.count(at) && it.score_row % 16 == 0 && x - it.score_from < it.score_row, "place of a product");
+          place[at] = {p.lists[it.tokens + (it.row0 + r) / G] * G + (it.row0 + r) % G, x};
+        }
+    }
+    std::vector<std::map<int, int>> summed((size_t)n);
+    for (const auto& it : p.sitems) {
+      CHECK(it.k1 - it.k0 <= p.kScoreKeys && (it.k0 - it.score_from) % 4 == 0 && it.rows == ql[it.req] * G, "score item");
+      for (int x = it.k0; x < it.k1; x++) {
+        summed[it.req][x]++;
+        for (int r = 0; r < it.rows; r++) {
+          const auto f = place.find((int64_t)it.score * 16 + (int64_t)(it.row0 + r) * it.score_row + x - it.score_from);
+          CHECK(f != place.end() && f->second == std::make_pair(p.q_first[it.req] * G + r, x), "product of row %d, key %d", r, x);
+        }
+      }
+    }
+    for (const auto& it : p.wrest)
+      for (int x = it.k0; x < it.k1; x++) summed[it.req][x]++;
+    for (int i = 0; i < n; i++) {
+      CHECK((int)summed[i].size() == (ql[i] ? len[i] : 0), "keys of %d summed", i);
+      for (auto& k : summed[i]) CHECK(k.second == 1 && k.first < len[i], "key %d of %d summed %d times", k.first, i, k.second);
+    }
     // weight items: every key of a request with rows once
     std::vector<std::map<int, int>> w((size_t)n);
     for (const auto& it : p.witems) {
