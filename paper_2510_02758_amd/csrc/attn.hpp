@@ -70,7 +70,7 @@ struct JoinArgs {
 struct WeightArgs {
   AttnArgs a;
   const kvswap::WeightItem* items;
-  const int32_t *q_first, *off;
+  const int32_t *q_first, *reqs;
   const float* lse;
   int64_t lse_ts;
   float* weights;

@@ -29,9 +29,10 @@ struct AttnItem {
   // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
   int32_t score, score_row, score_from, pad;
 };
-// One piece of weight accumulation: keys [k0, k1) of a request, whose products are computed again.
+// One piece of weight accumulation whose products are computed again: keys [k0, k1) that `count` requests have in common, for the
+// rows of these, requests wreqs[first ..].
 struct WeightItem {
-  int32_t req, k0, k1, pad;
+  int32_t table, k0, k1, first, count, pad[3];
 };
 // The same from products that were kept: the request's rows are row0 .. row0+rows-1 of their tile.
 struct ScoreItem {
@@ -68,6 +69,7 @@ class BatchPlan {
   std::vector<int32_t> join_off, join;                       // per token: partial rows of its first query head
   // Weights: of all keys from products computed again; or of row tiles' keys from kept ones, and of the others computed again.
   std::vector<WeightItem> witems, wrest;
+  std::vector<int32_t> wreqs;
   std::vector<ScoreItem> sitems;
   int64_t scores = 0;                                        // kept products of one KV head
   int32_t partial_rows = 0, most_parts = 0;
@@ -76,7 +78,7 @@ class BatchPlan {
   // Entries of the table that an item may need: its part of the table is held on chip.
   static constexpr int32_t kMaxEntries = 2048;
   static constexpr int32_t kRowTile = 16;
-  static constexpr int32_t kWeightKeys = 512, kScoreKeys = 1024;
+  static constexpr int32_t kWeightKeys = 128, kWeightReqs = 32, kScoreKeys = 1024;
 
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
           const BatchShape& s) {
@@ -163,7 +165,6 @@ class BatchPlan {
     T = rows;
     find_nodes(s.B);
     cut(s);
-    cut_weights();
   }
 
   // Blocks of request i that every one of its rows sees whole.
@@ -250,6 +251,8 @@ class BatchPlan {
     huge_.clear();
     uses_.clear();
     wrest.clear();
+    witems.clear();
+    wreqs.clear();
     sitems.clear();
     scores = 0;
     seen_.assign((size_t)T, 0);
@@ -297,9 +300,13 @@ class BatchPlan {
         for (int64_t r = 0; r < rows; r += s.big_tile)
           huge_.push_back(tile(0, tokens, (int32_t)r, (int32_t)std::min<int64_t>(s.big_tile, rows - r)));
       }
-      if (rows > kRowTile)
-        for (int32_t i : node.reqs)
-          for (int32_t k = node.from; k < node.to; k += kWeightKeys) wrest.push_back({i, k, std::min(node.to, k + kWeightKeys), 0});
+      const int32_t reqs = (int32_t)node.reqs.size(), first = (int32_t)wreqs.size();
+      wreqs.insert(wreqs.end(), node.reqs.begin(), node.reqs.end());
+      for (int32_t k = node.from; k < node.to; k += kWeightKeys)
+        for (int32_t r = 0; r < reqs; r += kWeightReqs) {
+          witems.push_back({off[node.reqs[0]], k, std::min(node.to, k + kWeightKeys), first + r, std::min(kWeightReqs, reqs - r), {}});
+          if (rows > kRowTile) wrest.push_back(witems.back());
+        }
       for (size_t j = list; j < lists.size(); j++)
         if (node.to > node.from) seen_[lists[j]]++;
     }
@@ -431,12 +438,6 @@ class BatchPlan {
         }
       k = e;
     }
-  }
-
-  void cut_weights() {
-    witems.clear();
-    for (int32_t i = 0; i < n; i++)
-      for (int32_t k = 0; q_len[i] && k < len[i]; k += kWeightKeys) witems.push_back({i, k, std::min(len[i], k + kWeightKeys), 0});
   }
 };
 

@@ -37,7 +37,7 @@ struct kv_batch {
   hipEvent_t up_ev[2] = {nullptr, nullptr};
   bool up_busy[2] = {false, false};
   int turn = 0;
-  const int32_t *wg_items = nullptr, *wg_big = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
+  const int32_t *wg_items = nullptr, *wg_big = nullptr, *wreqs = nullptr, *table = nullptr, *off = nullptr, *len = nullptr, *q_first = nullptr, *limit = nullptr, *lists = nullptr,
                 *join_off = nullptr, *join = nullptr;
   const AttnItem* items = nullptr;
   const WeightItem *witems = nullptr, *wrest = nullptr;
@@ -244,7 +244,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     const void** at;
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
-  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems), VEC(pl.wrest, b->wrest), VEC(pl.sitems, b->sitems),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
+  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems), VEC(pl.wrest, b->wrest), VEC(pl.sitems, b->sitems), VEC(pl.wreqs, b->wreqs),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
                         VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
                         VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
 #undef VEC
@@ -482,7 +482,7 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   }
   const std::vector<WeightItem>& again = keeps ? pl.wrest : pl.witems;
   if (a->weights && !again.empty()) {
-    WeightArgs w{k, keeps ? b->wrest : b->witems, b->q_first, b->off, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
+    WeightArgs w{k, keeps ? b->wrest : b->witems, b->q_first, b->wreqs, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
     f16 ? launch_weights<_Float16>(fp8, w, (int)again.size(), st) : launch_weights<__bf16>(fp8, w, (int)again.size(), st);
     OPCHK(b, hipGetLastError());
   }

@@ -147,7 +147,8 @@ int main(int argc, char** argv) {
       }
     }
     for (const auto& it : p.wrest)
-      for (int x = it.k0; x < it.k1; x++) summed[it.req][x]++;
+      for (int k = it.first; k < it.first + it.count; k++)
+        for (int x = it.k0; x < it.k1; x++) summed[p.wreqs[k]][x]++;
     for (int i = 0; i < n; i++) {
       CHECK((int)summed[i].size() == (ql[i] ? len[i] : 0), "keys of %d summed", i);
       for (auto& k : summed[i]) CHECK(k.second == 1 && k.first < len[i], "key %d of %d summed %d times", k.first, i, k.second);
@@ -155,8 +156,12 @@ int main(int argc, char** argv) {
     // weight items: every key of a request with rows once
     std::vector<std::map<int, int>> w((size_t)n);
     for (const auto& it : p.witems) {
-      CHECK(it.k1 > it.k0 && (it.k1 - 1) / s.B - it.k0 / s.B + 1 <= kvswap::BatchPlan::kMaxEntries, "weight item");
-      for (int x = it.k0; x < it.k1; x++) w[it.req][x]++;
+      CHECK(it.k1 > it.k0 && it.k1 - it.k0 <= p.kWeightKeys && it.count >= 1 && it.first + it.count <= (int)p.wreqs.size(), "weight item");
+      for (int k = it.first; k < it.first + it.count; k++)
+        for (int x = it.k0; x < it.k1; x++) {
+          CHECK(p.ids[it.table + x / s.B] == ids[off[p.wreqs[k]] + x / s.B], "block of key %d of %d", x, p.wreqs[k]);
+          w[p.wreqs[k]][x]++;
+        }
     }
     for (int i = 0; i < n; i++) {
       CHECK((int)w[i].size() == (ql[i] ? len[i] : 0), "weights of %d", i);
