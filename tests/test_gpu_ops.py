@@ -628,3 +628,14 @@ def test_evict_with_a_shared_prefix(gpu):
     shared = torch.from_numpy(rows[0][:3]).long().to(gpu)
     assert torch.equal(p.bits()[:, :, shared], before[:, :, shared])
     assert not torch.equal(p.bits(), before)
+
+
+def test_the_streaming_example(gpu):
+    """Append, attention over a shared prefix, eviction and the swap in one loop: a request that was preempted and resumed into other blocks
+    goes on as if it had not been.  Its prefix is no longer shared, so sums are taken in another order: 16-bit roundings apart."""
+    from paper_2510_02758_amd import stream_demo
+    kept, evicted, share = stream_demo.run()
+    plain, again, _ = stream_demo.run(preempt_at=-1)
+    assert evicted == again > 0 and share < 0.75
+    assert kept.isfinite().all() and plain.isfinite().all()
+    assert float((kept - plain).norm() / plain.norm()) < 0.05
