@@ -219,7 +219,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   int rc = kvswap::pool_usable(b->pool);
   if (rc) return rc;
   hipStream_t st = (hipStream_t)stream;
-  if (!b->v.plan_only && is_capturing(st)) return KV_EINVAL;
+  if (!b->v.plan_only && (is_capturing(st) || (b->used && b->last != st && is_capturing(b->last)))) return KV_EINVAL;
   BatchPlan& pl = b->plan;
   kvswap::BatchShape shape;
   shape.H = b->v.H;
@@ -235,6 +235,13 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   b->max_len = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);
   if (b->v.plan_only) return KV_OK;
+  // a failure from here on leaves a batch that describes nothing: the device does not have what the plan says
+  struct Undo {
+    BatchPlan* pl;
+    ~Undo() {
+      if (pl) pl->n = pl->T = 0;
+    }
+  } undo{&pl};
   rc = order(b, st);
   if (rc) return rc;
 
@@ -254,13 +261,6 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   const size_t prows = (size_t)pl.partial_rows * H, lse_n = (size_t)pl.T * H * pl.G;
   const size_t ws_need = padded(prows * b->v.D * 4) + padded(prows * sizeof(float2)) + padded(lse_n * 4);
   const int k = b->turn;
-  // a failure from here on leaves a batch that describes nothing
-  struct Undo {
-    BatchPlan* pl;
-    ~Undo() {
-      if (pl) pl->n = pl->T = 0;
-    }
-  } undo{&pl};
   if (need > b->mem_cap) {
     rc = drain(b);
     if (rc) return rc;

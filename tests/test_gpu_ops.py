@@ -259,6 +259,31 @@ def test_rows_do_not_feel_tokens_that_they_do_not_see_in_any_kernel(gpu, dtype, 
             assert (np.abs(got[j] - ref[j]) <= tol[j]).all(), j
 
 
+@pytest.mark.parametrize("size", [1e-4, 2000.0])
+@pytest.mark.parametrize("io_name", ["f16", "bf16"])
+@pytest.mark.parametrize("B,q_lens", [(16, [1, 1]), (5, [1, 1]), (16, [60, 1]), (5, [60, 1])])
+def test_scales_far_from_one(gpu, B, q_lens, io_name, size):
+    """fp8 values with scales that weights times scale in f16 would not survive; blocks differ by a factor of up to eight."""
+    import torch
+    lens, H, G, D = [300, 70], 2, 4, 64
+    N = sum(-(-n // B) for n in lens) + 3
+    p = Pool(gpu, W.Geometry(1, H, D, B, "fp8_e4m3", N, scales=True), seed=11)
+    rows = _tables(p.rng, N, lens, B)
+    p.fill(rows, lens)
+    small = torch.randn(2, N, B, H, D, generator=torch.Generator().manual_seed(1)).clamp_(-4, 4)
+    used = ~torch.isnan(p.view[0].float())
+    p.bits()[0] = torch.where(used, small.to(gpu).to(torch.float8_e4m3fn).view(torch.uint8), p.bits()[0])
+    p.scale[0, 0].uniform_(0.5, 1.0)
+    p.scale[0, 1].uniform_(size / 8, size)
+    q = torch.from_numpy(p.rng.standard_normal((sum(q_lens), G * H, D))).to(_torch_type(io_name)).to(gpu)
+    o, ids = R.csr(rows)
+    out = torch.empty_like(q)
+    kv.kv_check(p.batch.set(o, ids, lens, q_lens, G * H))
+    kv.kv_check(p.batch.attn(0, q, out, D ** -0.5))
+    ref, tol, _, _, _, _ = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), D ** -0.5, io_name, B)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol + 2.0 ** -25).all()
+
+
 def test_a_negative_scale_and_none(gpu):
     import torch
     for lens, q_lens in (([300, 70], [1, 1]), ([300, 70], [80, 1])):
