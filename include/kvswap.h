@@ -414,8 +414,8 @@ const char* kv_strerror(int code);
  * All calls go to a stream of the caller's (the compute stream), not to the evict or load stream: transfers that touch the same
  * blocks are ordered by the caller, through wait_event, kv_sync and kv_req_wait.  They are asynchronous, check everything before
  * they enqueue anything, and read host arrays during the call.  All pointers in the argument structures are device
- * pointers unless they say otherwise; strides there count elements, the innermost dimension is contiguous.  Queries, keys, values and outputs are of
- * the batch's io type: KV_F16 or KV_BF16, the pool's own where the pool is of one of these.
+ * pointers unless they say otherwise; strides there count elements, the innermost dimension is contiguous.  Queries, keys, values and
+ * outputs are of the call's io_dtype: KV_F16 or KV_BF16, the pool's own where the pool is of one of these.
  *
  * kv_batch: the requests of one step, set once and used by the calls of all layers.  Request i of n has num_tokens[i] tokens
  * in the cache, the last q_lens[i] of them new in this step: these are the T = sum of q_lens rows of the tensors, request by
@@ -426,8 +426,9 @@ const char* kv_strerror(int code);
 typedef struct kv_batch kv_batch; /* opaque */
 
 /* A batch on the pool; the pool must outlive it (KV_EINVAL: a head_dim that is no multiple of 8, above 128 none of 16, or above 256).
- * The batch owns device memory for the tables, the plan of the attention
- * and its partial results, which kv_batch_set allocates as batches grow. */
+ * The batch owns device memory for the tables, the plan of the attention and its partial results, which kv_batch_set allocates as
+ * batches grow, and from the first kv_attn with weights on for products, which grows then with the batches (4 bytes for each of a
+ * row tile's up to 16 rows and its keys; a call in a capture takes none and computes products twice instead). */
 int kv_batch_create(kv_pool* p, kv_batch** out);
 /* Waits for the batch's work, then frees it. */
 int kv_batch_destroy(kv_batch* b);

@@ -315,7 +315,7 @@ class BatchPlan {
     for (const Tile& t : few_) work += std::max(t.limit - nodes_[t.node].from, 0);
     // Where there is enough for every workgroup, its four wavefronts take four heads (two, if the head count is no multiple of four) rather
     // than four runs of one head's keys: they then read neighbouring bytes at the same time.  64 requests of 512 to 4096 tokens with 8
-    // heads of 128 in bf16: 106 us instead of 134, 32 requests of 256 to 8192 with 32 heads in fp8: 188 instead of 209.
+    // heads of 128 in bf16: 103 us instead of 135, 32 requests of 256 to 8192 with 32 heads in fp8: 175 to 181 instead of 207.
     heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
     wg_items.clear();
     deal_out(few_, s.wgs * heads / s.H, s.least / heads, s.B, &wg_items, &mixed);
@@ -365,9 +365,9 @@ class BatchPlan {
     return part;
   }
 
-  // Tiles of whole tokens.  If one piece of at most `share` keys for each of the workgroups that are to run at a time (`held`) is enough, every tile is cut by
-  // itself, and each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares: a workgroup may take
-  // the end of one tile, whole ones and the beginning of another.
+  // Tiles of whole tokens.  If one piece of at most `share` keys for each of the workgroups that are to run at a time (`held`) is enough,
+  // every tile is cut by itself, and each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares:
+  // a workgroup may take the end of one tile, whole ones and the beginning of another.
   void deal_out(const std::vector<Tile>& tiles, int64_t held, int64_t least, int32_t B, std::vector<int32_t>* wgs, bool* any_mixed) {
     int64_t work = 0;
     for (const Tile& t : tiles) work += std::max(t.limit - nodes_[t.node].from, 0);
@@ -376,7 +376,7 @@ class BatchPlan {
     int64_t share = std::max<int64_t>(least, (work + held - 1) / held);
     share = std::min(most, (share + kStep - 1) / kStep * kStep);
     // Tiles that all have a workgroup of their own stay whole if the longest is not much longer than a share: partial results cost more
-    // (two prompts' chunks of 1024 and 517 tokens behind 8001 and 5000: 207 us whole, 219 in equal shares).
+    // (two prompts' chunks of 1024 and 517 tokens behind 8001 and 5000: 211 us whole, 214 in equal shares, and 100 MB of partial results).
     int64_t longest = 0;
     for (const Tile& t : tiles) longest = std::max<int64_t>(longest, t.limit - nodes_[t.node].from);
     if ((int64_t)tiles.size() <= held && longest <= share + share * 5 / 8 && longest <= most) share = std::max(share, longest);

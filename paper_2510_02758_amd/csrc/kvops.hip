@@ -1,6 +1,7 @@
 // C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction.
-// Host side of each call: check everything, then at most three launches on the caller's stream; nothing is allocated and nothing
-// waits outside kv_batch_create, kv_batch_set and kv_batch_destroy.
+// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict, for kv_attn one
+// or two for the tiles, one for their join and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set
+// and kv_batch_destroy, and nothing is allocated there but the room for kept products, when weights are first asked for.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -226,7 +227,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   shape.B = b->v.B;
   shape.N = b->v.N;
   // Two workgroups of row tiles a CU: with three, more places of the pool are read at a time, and each more slowly (64 requests of 512 to
-  // 4096 tokens on 8 heads of 128 in bf16: 106 us with two, 123 with three, 133 with one; 32 of 256 to 8192 on 32 heads in fp8: 189, 190, 246).
+  // 4096 tokens on 8 heads of 128 in bf16: 103 us with two, 122 with three, 140 with one; 32 of 256 to 8192 on 32 heads in fp8: 181, 185, 242).
   shape.wgs = b->v.cus * 2;
   shape.big_wgs = b->v.cus * (b->v.D <= 128 ? 2 : 1);
   shape.big_tile = big_tile(b->v.D);
