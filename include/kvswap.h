@@ -428,7 +428,9 @@ typedef struct kv_batch kv_batch; /* opaque */
 /* A batch on the pool; the pool must outlive it (KV_EINVAL: a head_dim that is no multiple of 8, above 128 none of 16, or above 256).
  * The batch owns device memory for the tables, the plan of the attention and its partial results, which kv_batch_set allocates as
  * batches grow, and from the first kv_attn with weights on for products, which grows then with the batches (4 bytes for each of a
- * row tile's up to 16 rows and its keys; a call in a capture takes none and computes products twice instead). */
+ * row tile's up to 16 rows and its keys; a call in a capture takes none and computes products twice instead).  So does kv_evict for
+ * the order of its moves (8 bytes for each layer, head and some 128 tokens of the longest request, times n; in a capture each head's
+ * moves are made one after the other instead). */
 int kv_batch_create(kv_pool* p, kv_batch** out);
 /* Waits for the batch's work, then frees it. */
 int kv_batch_destroy(kv_batch* b);

@@ -1,7 +1,7 @@
 // C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction.
 // Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict, for kv_attn one
 // or two for the tiles, one for their join and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set
-// and kv_batch_destroy, and nothing is allocated there but the room for kept products, when weights are first asked for.
+// and kv_batch_destroy, and nothing is allocated there but the room for kept products and for the order of moves, when they are first needed.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -55,6 +55,10 @@ struct kv_batch {
   float* scores = nullptr;
   size_t scores_cap = 0;
 
+  // Tickets of an eviction's chunks, taken when an eviction first needs them (and not in a capture).
+  int32_t* turns = nullptr;
+  size_t turns_cap = 0;
+
   // The stream of the newest work; another stream's call waits for what is on it.
   bool used = false;
   hipStream_t last = nullptr;
@@ -106,6 +110,24 @@ bool scores_room(kv_batch* b, hipStream_t st) {
     return false;
   }
   b->scores_cap = need + need / 4;
+  return true;
+}
+
+// Room for the tickets of an eviction's chunks.
+bool turns_room(kv_batch* b, size_t need, hipStream_t st) {
+  if (need <= b->turns_cap) return true;
+  if (is_capturing(st)) return false;
+  if (b->turns) {
+    (void)hipFree(b->turns);
+    b->turns = nullptr;
+    b->turns_cap = 0;
+  }
+  if (hipMalloc((void**)&b->turns, need + need / 4) != hipSuccess) {
+    (void)hipGetLastError();
+    b->turns = nullptr;
+    return false;
+  }
+  b->turns_cap = need + need / 4;
   return true;
 }
 
@@ -206,6 +228,7 @@ int kv_batch_destroy(kv_batch* b) try {
     if (b->mem) (void)hipFree(b->mem);
     if (b->ws) (void)hipFree(b->ws);
     if (b->scores) (void)hipFree(b->scores);
+    if (b->turns) (void)hipFree(b->turns);
   }
   delete b;
   return rc;
@@ -546,16 +569,28 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     k.group = v.B >= 64 ? v.B : 64 / v.B * v.B;
     k.first_tok = fixed_blocks * v.B;
     const unsigned heads = (unsigned)a->num_layers * pl.n * v.H;
+    // chunks of the move
+    constexpr int kU = 8;
+    const int32_t bytes = v.D * k.e, most = bytes % 16 ? 0 : std::min(kMoveRows, kU * (256 / (bytes / 16)));
+    k.rows = v.scale ? most / v.B * v.B : most;
+    bool apart = crowded && k.rows > 0;
+    if (apart) {
+      k.chunks = std::max(1, (a->keep - k.first_tok + k.rows - 1) / k.rows);
+      if (k.chunks > 1) {
+        // for any eviction of this batch: a captured one's room must not move before the next kv_batch_set
+        const size_t room = (size_t)v.L * pl.n * v.H * 2 * (2 + (size_t)b->max_len / k.rows) * 4;
+        apart = (int64_t)heads * 2 * k.chunks <= INT32_MAX && turns_room(b, room, st);
+        if (apart) k.turns = b->turns;
+      }
+    }
     hipLaunchKernelGGL(kv_evict_select_kernel, dim3(heads), dim3(kSelectLanes), 0, st, k);
     OPCHK(b, hipGetLastError());
     if (crowded) {
-      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(heads * 2), dim3(256), 0, st, k); };
-      if (v.scale)
-        go(kv_evict_move_scaled_kernel<true>);
-      else if (v.D * k.e % 16)
-        go(kv_evict_move_scaled_kernel<false>);
+      auto go = [&](auto kern, unsigned grid) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, k); };
+      if (apart)
+        v.scale ? go(kv_evict_move_kernel<true, kU>, heads * 2 * k.chunks) : go(kv_evict_move_kernel<false, kU>, heads * 2 * k.chunks);
       else
-        go(kv_evict_move_kernel<4>);
+        v.scale ? go(kv_evict_move_alone_kernel<true>, heads * 2) : go(kv_evict_move_alone_kernel<false>, heads * 2);
       OPCHK(b, hipGetLastError());
     }
   }
