@@ -583,7 +583,18 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
         if (apart) k.turns = b->turns;
       }
     }
-    hipLaunchKernelGGL(kv_evict_select_kernel, dim3(heads), dim3(kSelectLanes), 0, st, k);
+    // Lanes of a row's workgroup: 256; more where a few rows are longer than these have registers for; a wavefront, which waits for no
+    // other, where there are rows enough to fill the chip with and one has the registers.  With the few moves that keeping 8 tokens needs,
+    // 64 / 256 / 1024 lanes: 2048 rows of 300 to 500 tokens 25 / 35 / 131 us, 64 such 16 / 15 / 22, 160 rows of 1790 to 7026 94 / 42 / 25, 8192 of
+    // 5000 to 8000 490 / 494 / 585.
+    const bool many = heads > 4u * b->v.cus;
+    auto select = [&](auto kern, int lanes) { hipLaunchKernelGGL(kern, dim3(heads), dim3(lanes), 0, st, k); };
+    if (many && b->max_len <= 64 * kSelectEach)
+      select(kv_evict_select_kernel<64>, 64);
+    else if (!many && b->max_len > 256 * kSelectEach)
+      select(kv_evict_select_kernel<1024>, 1024);
+    else
+      select(kv_evict_select_kernel<256>, 256);
     OPCHK(b, hipGetLastError());
     if (crowded) {
       auto go = [&](auto kern, unsigned grid) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, k); };

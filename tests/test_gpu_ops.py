@@ -633,6 +633,64 @@ def test_evict(gpu, name, in_place):
     assert same.all()
 
 
+EVICT_CHUNKS = {
+    # as EVICT: rows enough for a wavefront each, and moves of many chunks
+    "many rows": ((12, 32, 64, 16, "bf16", False), [200, 37, 1000], 30, 4, 8, "ties"),
+    "many rows, special": ((12, 32, 64, 16, "f16", False), [200, 37, 1000], 170, 0, 1, "special"),
+    "d 256": ((2, 2, 256, 4, "f16", False), [3000, 2900], 1500, 0, 0, "random"),
+    "all but the first": ((2, 2, 128, 16, "bf16", False), [1000], 999, 0, 999, "random"),
+    "fp8 with scales": ((1, 2, 256, 16, "fp8_e4m3", True), [900, 400], 350, 13, 20, "random"),
+    "fp8 with scales, odd blocks": ((2, 2, 128, 20, "fp8_e4m3", True), [900, 400, 501], 500, 50, 0, "random"),
+    "fp8 with scales, blocks larger than a chunk": ((1, 2, 256, 144, "fp8_e4m3", True), [900, 400], 350, 13, 20, "random"),
+}
+
+
+@pytest.mark.parametrize("name", list(EVICT_CHUNKS))
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict_in_chunks(gpu, name, in_place, monkeypatch):
+    monkeypatch.setitem(EVICT, name, EVICT_CHUNKS[name])
+    test_evict(gpu, name, in_place)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8_e4m3"])
+def test_evict_first_in_a_graph(gpu, dtype):
+    """A capture that finds no room for the order of the moves makes them one after the other."""
+    import torch
+    B, H, D, lens, keep = 16, 2, 256, [700, 333], 300
+    p = Pool(gpu, W.Geometry(1, H, D, B, dtype, 70, scales=dtype == "fp8_e4m3"), seed=6)
+    rows = _tables(p.rng, 70, lens, B)
+    p.fill(rows, lens)
+    o, ids = R.csr(rows)
+    st = torch.cuda.Stream()
+    w = torch.rand(1, 2, H, 700, device=gpu)
+    w2, kept = torch.zeros_like(w), torch.zeros(1, 2, H, keep, dtype=torch.int32, device=gpu)
+    start, scale = p.bits().clone(), None if p.scale is None else p.scale.clone()
+    torch.cuda.synchronize()
+    kv.kv_check(p.batch.set(o, ids, lens, [1, 1], H, stream=st))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        kv.kv_check(p.batch.evict(0, 1, w, kept, keep, 4, 8, weights_out=w2, stream=st))
+
+    def result(run):
+        p.bits().copy_(start)
+        if scale is not None:
+            p.scale.copy_(scale)
+        w2.zero_()
+        kept.zero_()
+        torch.cuda.synchronize()
+        run()
+        torch.cuda.synchronize()
+        return [x.clone() for x in (p.bits(), w2, kept)] + ([] if scale is None else [p.scale.clone()])
+
+    want = result(lambda: kv.kv_check(p.batch.evict(0, 1, w, kept, keep, 4, 8, weights_out=w2, stream=st)))
+    assert not torch.equal(want[0], start)
+    for turn in range(3):
+        w.uniform_()
+        want = result(lambda: kv.kv_check(p.batch.evict(0, 1, w, kept, keep, 4, 8, weights_out=w2, stream=st)))
+        for a, b in zip(want, result(graph.replay)):
+            assert torch.equal(a, b), turn
+
+
 def test_evict_with_a_shared_prefix(gpu):
     """Requests that share blocks may be evicted as long as the shared ones stay whole."""
     import torch
