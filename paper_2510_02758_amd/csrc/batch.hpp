@@ -104,6 +104,8 @@ class BatchPlan {
     }
     // nothing fails from here on but allocation: a batch that could not be set describes nothing
     n = T = 0;
+    counted_ = false;
+    blocks_ = s.N;
     try {
       lay_out(n_, offsets, blocks, tokens, q_lens, g, (int32_t)rows, keys, (size_t)table, s);
     } catch (...) {
@@ -114,20 +116,29 @@ class BatchPlan {
   }
 
   // Would rewriting blocks [first_block, keep_blocks) of the requests with more than `keep` tokens reach a block that the batch has twice?
-  bool rewrites_shared(int32_t keep, int32_t first_block, int32_t keep_blocks) const {
-    std::vector<int32_t> sorted(ids);
-    std::sort(sorted.begin(), sorted.end());
+  // Which blocks these are is found out once for a batch, when it is first asked.
+  bool rewrites_shared(int32_t keep, int32_t first_block, int32_t keep_blocks) {
+    if (!counted_) {
+      twice_.resize(ids.size());
+      times_.resize((size_t)blocks_, 0);
+      for (int32_t id : ids) times_[id] += times_[id] < 2;
+      for (size_t k = 0; k < ids.size(); k++) twice_[k] = times_[ids[k]] > 1;
+      for (int32_t id : ids) times_[id] = 0;
+      counted_ = true;
+    }
     for (int32_t i = 0; i < n; i++) {
       if (len[i] <= keep) continue;
-      for (int32_t k = off[i] + first_block; k < off[i] + keep_blocks; k++) {
-        const auto r = std::equal_range(sorted.begin(), sorted.end(), ids[k]);
-        if (r.second - r.first > 1) return true;
-      }
+      for (int32_t k = off[i] + first_block; k < off[i] + keep_blocks; k++)
+        if (twice_[k]) return true;
     }
     return false;
   }
 
  private:
+  std::vector<uint8_t> times_, twice_;  // of a block (all 0 between calls), of an entry of ids: is its block there twice?
+  bool counted_ = false;
+  int64_t blocks_ = 0;
+
   struct Node {
     std::vector<int32_t> reqs;
     int32_t from, to;  // keys

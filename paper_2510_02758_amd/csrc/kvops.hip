@@ -521,7 +521,7 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
   int rc = kvswap::pool_usable(b->pool);
   if (rc) return rc;
   const PoolView& v = b->v;
-  const BatchPlan& pl = b->plan;
+  BatchPlan& pl = b->plan;
   if (a->layer < 0 || a->num_layers < 0 || a->layer > v.L - a->num_layers) return KV_EINVAL;
   if (a->keep_first < 0 || a->keep_last < 0 || (int64_t)a->keep_first + a->keep_last > a->keep) return KV_EINVAL;
   if (pl.n == 0 || a->num_layers == 0) return KV_OK;
