@@ -12,6 +12,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
+struct DivBy {
+  uint32_t mul, shift;
+};
+__device__ __forceinline__ uint32_t div_by(const DivBy& d, uint32_t x) {
+  return d.shift >= 32 ? x : (uint32_t)(((uint64_t)x * d.mul) >> 32) >> d.shift;
+}
+
 struct KvSide {
   const char* k;   // keys of the layer
   int64_t vk;      // from a key to its value, bytes
@@ -21,12 +28,10 @@ struct KvSide {
   int32_t row;     // bytes from a token's head to the next token's: H * D * e
   int32_t head;    // bytes of a head: D * e
   int32_t D, B;
-  uint32_t div_mul, div_shift;  // x / B
+  DivBy by_b;
 };
 
-__device__ __forceinline__ uint32_t div_by_b(const KvSide& s, uint32_t x) {
-  return s.div_shift >= 32 ? x : (uint32_t)(((uint64_t)x * s.div_mul) >> 32) >> s.div_shift;
-}
+__device__ __forceinline__ uint32_t div_by_b(const KvSide& s, uint32_t x) { return div_by(s.by_b, x); }
 
 struct AttnArgs {
   KvSide kv;
@@ -75,6 +80,7 @@ struct WeightArgs {
   int64_t lse_ts;
   float* weights;
   int64_t w_rs, w_hs;
+  DivBy by_g;
 };
 
 struct SumArgs {

@@ -151,11 +151,10 @@ int drain(kv_batch* b) {
 size_t padded(size_t bytes) { return (bytes + 63) / 64 * 64; }
 
 // x / B by a product for 0 <= x < 2^31.
-void set_division(KvSide* s, int32_t B) {
+DivBy division(int32_t B) {
   int sh = 0;
   while ((1ll << sh) < B) sh++;
-  s->div_shift = sh ? sh - 1 : 32;
-  s->div_mul = sh ? (uint32_t)(((1ull << (31 + sh)) + B - 1) / B) : 0;
+  return {sh ? (uint32_t)(((1ull << (31 + sh)) + B - 1) / B) : 0, (uint32_t)(sh ? sh - 1 : 32)};
 }
 
 KvSide side(const kv_batch* b, int32_t layer) {
@@ -172,7 +171,7 @@ KvSide side(const kv_batch* b, int32_t layer) {
   s.head = v.D * e;
   s.D = v.D;
   s.B = v.B;
-  set_division(&s, v.B);
+  s.by_b = division(v.B);
   return s;
 }
 
@@ -506,7 +505,8 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   }
   const std::vector<WeightItem>& again = keeps ? pl.wrest : pl.witems;
   if (a->weights && !again.empty()) {
-    WeightArgs w{k, keeps ? b->wrest : b->witems, b->q_first, b->wreqs, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1]};
+    WeightArgs w{k, keeps ? b->wrest : b->witems, b->q_first, b->wreqs, k.lse, k.lse_ts, a->weights, a->weights_strides[0], a->weights_strides[1],
+                 division(pl.G)};
     f16 ? launch_weights<_Float16>(fp8, w, (int)again.size(), st) : launch_weights<__bf16>(fp8, w, (int)again.size(), st);
     OPCHK(b, hipGetLastError());
   }
