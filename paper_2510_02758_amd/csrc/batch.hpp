@@ -78,7 +78,7 @@ class BatchPlan {
   // Entries of the table that an item may need: its part of the table is held on chip.
   static constexpr int32_t kMaxEntries = 2048;
   static constexpr int32_t kRowTile = 16;
-  static constexpr int32_t kWeightKeys = 128, kWeightReqs = 32, kScoreKeys = 1024;
+  static constexpr int32_t kWeightKeys = 256, kWeightReqs = 16, kScoreKeys = 1024;
 
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
           const BatchShape& s) {
