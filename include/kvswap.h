@@ -430,14 +430,16 @@ typedef struct kv_batch kv_batch; /* opaque */
  * batches grow, and from the first kv_attn with weights on for products, which grows then with the batches (4 bytes for each of a
  * row tile's up to 16 rows and its keys; a call in a capture takes none and computes products twice instead).  So does kv_evict for
  * the order of its moves (8 bytes for each layer, head and some 128 tokens of the longest request, times n; in a capture each head's
- * moves are made one after the other instead). */
+ * moves are always made one after the other instead). */
 int kv_batch_create(kv_pool* p, kv_batch** out);
-/* Waits for the batch's work, then frees it. */
+/* Waits for the batch's work (for the device, if calls have been captured since the batch was set), then frees it. */
 int kv_batch_destroy(kv_batch* b);
 /* Replaces what the batch describes.  num_q_heads is a multiple of H: query head hq reads KV head hq / (num_q_heads / H).
  * The copies are enqueued on `stream`; earlier calls with the batch on other streams are waited for on the device, as is the
  * copy by later calls on other streams.  `stream` must not be capturing; kv_append, kv_attn and kv_evict may be captured on
- * the stream the batch was set on, and a replay is good until the next kv_batch_set.
+ * the stream the batch was set on, and a replay is good until the next kv_batch_set.  The batch does not see when a replay runs, and on
+ * which stream.  kv_batch_set and kv_batch_destroy therefore wait on the host for the device if calls have been captured since the batch was
+ * set.  Until then the caller keeps replays apart from each other and from direct calls with the batch: they use the same workspaces.
  * Errors: KV_EINVAL (negative sizes, q_lens[i] > num_tokens[i] except 1 row for 0 tokens, a row too short, a head count that does
  * not fit, a capturing stream), KV_ERANGE (block id): the batch stays as it was; KV_ENOMEM, KV_EHIP: it has no requests. */
 int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens,

@@ -55,7 +55,7 @@ struct kv_batch {
   float* scores = nullptr;
   size_t scores_cap = 0;
 
-  // Tickets of an eviction's chunks, taken when an eviction first needs them (and not in a capture).
+  // Tickets of an eviction's chunks, taken when an eviction first needs them; none in a capture.
   int32_t* turns = nullptr;
   size_t turns_cap = 0;
 
@@ -63,6 +63,7 @@ struct kv_batch {
   bool used = false;
   hipStream_t last = nullptr;
   hipEvent_t ev = nullptr;
+  bool captured = false;  // a capture has taken calls since the batch was set: replays may be under way on any stream
 };
 
 namespace {
@@ -94,6 +95,15 @@ bool is_capturing(hipStream_t st) {
   return hipStreamIsCapturing(st, &s) != hipSuccess || s != hipStreamCaptureStatusNone;
 }
 
+// While it lives, calls that wait do not invalidate a capture that another thread is at (in the global mode).
+struct Relaxed {
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  const bool changed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+  ~Relaxed() {
+    if (changed) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  }
+};
+
 // Room for the batch's kept products; false: there is none, they have to be computed again.
 bool scores_room(kv_batch* b, hipStream_t st) {
   const size_t need = (size_t)b->plan.scores * b->v.H * 4;
@@ -113,10 +123,11 @@ bool scores_room(kv_batch* b, hipStream_t st) {
   return true;
 }
 
-// Room for the tickets of an eviction's chunks.
+// Room for the tickets of an eviction's chunks.  None in a capture: two launches that drew from the same tickets at a time would leave
+// chunks out and wait for these, and when a replay runs is not known here.
 bool turns_room(kv_batch* b, size_t need, hipStream_t st) {
-  if (need <= b->turns_cap) return true;
   if (is_capturing(st)) return false;
+  if (need <= b->turns_cap) return true;
   if (b->turns) {
     (void)hipFree(b->turns);
     b->turns = nullptr;
@@ -133,13 +144,24 @@ bool turns_room(kv_batch* b, size_t need, hipStream_t st) {
 
 // Puts `st` behind the batch's work on another stream.
 int order(kv_batch* b, hipStream_t st) {
+  const bool capturing = is_capturing(st);
   if (b->used && b->last != st) {
-    if (is_capturing(st) || is_capturing(b->last)) return KV_EINVAL;
+    if (capturing || is_capturing(b->last)) return KV_EINVAL;
     OPCHK(b, hipEventRecord(b->ev, b->last));
     OPCHK(b, hipStreamWaitEvent(st, b->ev, 0));
   }
   b->used = true;
   b->last = st;
+  b->captured = b->captured || capturing;
+  return KV_OK;
+}
+
+// Waits for replays of captured calls, which may be on any stream, before what they read is changed or freed.
+int settle(kv_batch* b) {
+  if (!b->captured) return KV_OK;
+  Relaxed relaxed;
+  OPCHK(b, hipDeviceSynchronize());
+  b->captured = false;
   return KV_OK;
 }
 
@@ -219,7 +241,8 @@ int kv_batch_destroy(kv_batch* b) try {
   if (!b) return KV_EINVAL;
   int rc = KV_OK;
   if (!b->v.plan_only) {  // (the pool may be gone: it is not touched)
-    if (b->used && hipStreamSynchronize(b->last) != hipSuccess) rc = KV_EHIP;
+    Relaxed relaxed;
+    if (b->captured ? hipDeviceSynchronize() != hipSuccess : b->used && hipStreamSynchronize(b->last) != hipSuccess) rc = KV_EHIP;
     for (hipEvent_t e : {b->ev, b->up_ev[0], b->up_ev[1]})
       if (e) (void)hipEventDestroy(e);
     for (char* u : b->up)
@@ -244,6 +267,11 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   hipStream_t st = (hipStream_t)stream;
   if (!b->v.plan_only && (is_capturing(st) || (b->used && b->last != st && is_capturing(b->last)))) return KV_EINVAL;
   BatchPlan& pl = b->plan;
+  rc = settle(b);
+  if (rc) {
+    pl.n = pl.T = 0;
+    return rc;
+  }
   kvswap::BatchShape shape;
   shape.H = b->v.H;
   shape.B = b->v.B;
@@ -577,7 +605,7 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     if (apart) {
       k.chunks = std::max(1, (a->keep - k.first_tok + k.rows - 1) / k.rows);
       if (k.chunks > 1) {
-        // for any eviction of this batch: a captured one's room must not move before the next kv_batch_set
+        // for any eviction of this batch
         const size_t room = (size_t)v.L * pl.n * v.H * 2 * (2 + (size_t)b->max_len / k.rows) * 4;
         apart = (int64_t)heads * 2 * k.chunks <= INT32_MAX && turns_room(b, room, st);
         if (apart) k.turns = b->turns;

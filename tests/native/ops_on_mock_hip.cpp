@@ -1,0 +1,198 @@
+// The host side of the operators on the pool's contents (kvops.hip, unchanged) on the stand-in HIP runtime: order between calls, captures and
+// replays, workspaces, launches.  Kernels are not run; a launch is an operation in its stream that notes what it would have read.
+//
+// usage: ops_on_mock_hip NAME   (one of the checks in main; prints "ok")
+#include "mock_device.h"
+
+#include <cstdio>
+#include <string>
+
+struct Launched {
+  std::string kernel;
+  dim3 grid, block;
+  const void* turns;
+  int32_t first_len;  // the batch's first length, as the launch found it in the tables when it ran (evictions)
+  bool ran;
+};
+static std::vector<Launched> launched;
+
+#undef hipLaunchKernelGGL
+#define hipLaunchKernelGGL(kern, grid, block, lds_bytes, stream, ...) record(#kern, (grid), (block), (stream), __VA_ARGS__)
+template <class Args, class... More>
+void record(const char* kernel, dim3 grid, dim3 block, hipStream_t st, const Args& a, const More&...);
+
+#include "kvops.hip"
+
+template <class Args, class... More>
+void record(const char* kernel, dim3 grid, dim3 block, hipStream_t st, const Args& a, const More&...) {
+  const size_t at = launched.size();
+  launched.push_back({kernel, grid, block, nullptr, -1, false});
+  const int32_t* len = nullptr;
+  if constexpr (std::is_same_v<Args, EvictArgs>) {
+    launched[at].turns = a.turns;
+    len = a.len;
+  }
+  mockhip::enqueue(st, [at, len] {
+    launched[at].ran = true;
+    if (len) launched[at].first_len = len[0];
+  });
+}
+
+// The attention's tiles are in files of their own.
+static std::vector<int32_t> tables_seen;
+template <typename E>
+void launch_attn(bool, const AttnArgs& a, const kvswap::BatchPlan&, hipStream_t st) {
+  const int32_t* table = a.table;
+  mockhip::enqueue(st, [table] { tables_seen.push_back(table[0]); });
+}
+template <typename E>
+void launch_join(const JoinArgs&, const kvswap::BatchPlan&, hipStream_t) {}
+template <typename E>
+void launch_weights(bool, const WeightArgs&, int, hipStream_t) {}
+template void launch_attn<__bf16>(bool, const AttnArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_attn<_Float16>(bool, const AttnArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_join<__bf16>(const JoinArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_join<_Float16>(const JoinArgs&, const kvswap::BatchPlan&, hipStream_t);
+template void launch_weights<__bf16>(bool, const WeightArgs&, int, hipStream_t);
+template void launch_weights<_Float16>(bool, const WeightArgs&, int, hipStream_t);
+
+// A pool handle as far as the operators look at one.
+struct kv_pool {
+  kvswap::PoolView v;
+  int last_hip = 0;
+};
+namespace kvswap {
+int pool_view(kv_pool* p, PoolView* out) { return *out = p->v, KV_OK; }
+int pool_usable(kv_pool*) { return KV_OK; }
+void pool_hip_error(kv_pool* p, int code) { p->last_hip = code; }
+int pool_may_rewrite(kv_pool*, int32_t, const uint64_t*) { return KV_OK; }
+void pool_rewritten(kv_pool*, int32_t, const uint64_t*, const int32_t*) {}
+}  // namespace kvswap
+
+#define CHECK(cond)                                                      \
+  do {                                                                   \
+    if (!(cond)) {                                                       \
+      std::printf("FAILED %s:%d: %s\n", __FILE__, __LINE__, #cond);      \
+      std::exit(1);                                                      \
+    }                                                                    \
+  } while (0)
+
+namespace {
+
+char* const kSomewhere = (char*)(uintptr_t)4096;  // stands for device memory that nothing here touches
+
+struct World {
+  kv_pool pool;
+  hipStream_t s[3];
+  kv_batch* b = nullptr;
+  explicit World(int32_t L = 2, int32_t H = 2, int32_t D = 128, int32_t B = 16, int64_t N = 1 << 20) {
+    mockhip::reset(1);
+    const int64_t chunk = (int64_t)B * H * D * 2;
+    pool.v = kvswap::PoolView{L, H, D, B, KV_BF16, N, kSomewhere, 2 * N * chunk, N * chunk, chunk, nullptr, 0, 0, 0, false, false, 256};
+    for (hipStream_t& x : s) {
+      CHECK(hipStreamCreateWithFlags(&x, hipStreamNonBlocking) == hipSuccess);
+      all_streams.push_back(x);
+    }
+    mockhip::set_policy(mockhip::kLazy, nullptr);  // nothing runs before somebody waits for it
+    CHECK(kv_batch_create(&pool, &b) == KV_OK);
+  }
+  // n requests of `tokens` tokens in blocks of their own, from block `first` on
+  int set(hipStream_t st, int32_t n, int32_t tokens, int32_t first = 0) {
+    std::vector<int32_t> off{0}, ids, len, q;
+    for (int32_t i = 0; i < n; i++) {
+      for (int32_t k = 0; k < (tokens + pool.v.B - 1) / pool.v.B; k++) ids.push_back(first + (int32_t)ids.size());
+      off.push_back((int32_t)ids.size());
+      len.push_back(tokens);
+      q.push_back(1);
+    }
+    return kv_batch_set(b, n, off.data(), ids.data(), len.data(), q.data(), pool.v.H, st);
+  }
+  int attn(hipStream_t st, bool weights = false) {
+    kv_attn_args a{};
+    a.struct_size = sizeof(a);
+    a.io_dtype = KV_BF16;
+    a.scale = 1.f;
+    a.q = a.out = kSomewhere;
+    if (weights) {
+      a.weights = (float*)kSomewhere;
+      a.weights_cap = 1 << 30;
+    }
+    return kv_attn(b, &a, st);
+  }
+  int append(hipStream_t st) {
+    kv_append_args a{};
+    a.struct_size = sizeof(a);
+    a.io_dtype = KV_BF16;
+    a.k = a.v = kSomewhere;
+    return kv_append(b, &a, st);
+  }
+  int evict(hipStream_t st, int32_t keep) {
+    kv_evict_args a{};
+    a.struct_size = sizeof(a);
+    a.num_layers = pool.v.L;
+    a.keep = keep;
+    a.weights = (const float*)kSomewhere;
+    a.kept = (int32_t*)kSomewhere;
+    a.weights_cap = 1 << 30;
+    return kv_evict(b, &a, st);
+  }
+  ~World() {
+    for (hipStream_t x : s) CHECK(hipStreamSynchronize(x) == hipSuccess);
+    if (b) CHECK(kv_batch_destroy(b) == KV_OK);
+    for (hipStream_t x : s) CHECK(hipStreamDestroy(x) == hipSuccess);
+    all_streams.clear();
+  }
+};
+
+// A replay that is under way on another stream reads the tables it was captured with: a new batch, or the end of this one, comes after it.
+void replay_then_set() {
+  World w;
+  CHECK(w.set(w.s[0], 3, 40, 100) == KV_OK);
+  CHECK(hipStreamSynchronize(w.s[0]) == hipSuccess);
+  mockhip::begin_capture(w.s[0]);
+  CHECK(w.attn(w.s[0]) == KV_OK);
+  const mockhip::Graph g = mockhip::end_capture();
+  mockhip::replay(w.s[1], g);
+  mockhip::replay(w.s[1], g);
+  CHECK(tables_seen.empty());
+  CHECK(w.set(w.s[0], 3, 40, 500) == KV_OK);
+  CHECK(hipStreamSynchronize(w.s[0]) == hipSuccess);  // the new tables are there
+  CHECK(hipStreamSynchronize(w.s[1]) == hipSuccess);
+  CHECK((tables_seen == std::vector<int32_t>{100, 100}));
+  // without a capture since, nothing waits for the device
+  CHECK(device_waits == 1 && w.attn(w.s[0]) == KV_OK && w.set(w.s[0], 3, 40, 900) == KV_OK && device_waits == 1);
+  mockhip::begin_capture(w.s[0]);
+  CHECK(w.attn(w.s[0]) == KV_OK);
+  const mockhip::Graph g2 = mockhip::end_capture();
+  CHECK(hipStreamSynchronize(w.s[0]) == hipSuccess);
+  tables_seen.clear();
+  mockhip::replay(w.s[2], g2);
+  CHECK(kv_batch_destroy(w.b) == KV_OK);
+  w.b = nullptr;
+  CHECK((tables_seen == std::vector<int32_t>{900}));
+}
+
+// Tickets are for direct calls alone, also once there is room for them.
+void captures_draw_no_tickets() {
+  World w;
+  CHECK(w.set(w.s[0], 2, 4000) == KV_OK);
+  CHECK(w.evict(w.s[0], 2000) == KV_OK);
+  CHECK(launched.size() == 2 && launched[1].turns);
+  mockhip::begin_capture(w.s[0]);
+  CHECK(w.evict(w.s[0], 2000) == KV_OK);
+  mockhip::end_capture();
+  CHECK(launched.size() == 4 && !launched[2].turns && !launched[3].turns && launched[3].grid.x == 2u * 2 * 2 * 2);
+  CHECK(w.evict(w.s[0], 2000) == KV_OK);
+  CHECK(launched.size() == 6 && launched[5].turns);
+}
+
+}  // namespace
+
+int main(int, char** argv) {
+  const std::string name = argv[1];
+  if (name == "replay_then_set") replay_then_set();
+  else if (name == "captures_draw_no_tickets") captures_draw_no_tickets();
+  else return 2;
+  std::printf("ok\n");
+  return 0;
+}
