@@ -142,7 +142,8 @@ bool turns_room(kv_batch* b, size_t need, hipStream_t st) {
   return true;
 }
 
-// Puts `st` behind the batch's work on another stream.
+// Puts `st` behind the batch's work on another stream.  The checks behind the launches read the thread's last HIP error, which any earlier
+// call of the application may have left behind (an event query that said "not ready" is enough): it is cleared first.
 int order(kv_batch* b, hipStream_t st) {
   const bool capturing = is_capturing(st);
   if (b->used && b->last != st) {
@@ -153,6 +154,7 @@ int order(kv_batch* b, hipStream_t st) {
   b->used = true;
   b->last = st;
   b->captured = b->captured || capturing;
+  (void)hipGetLastError();
   return KV_OK;
 }
 

@@ -186,12 +186,29 @@ void captures_draw_no_tickets() {
   CHECK(launched.size() == 6 && launched[5].turns);
 }
 
+// An error that another part of the program has left behind is none of the call's: an eviction would stop between its two launches.
+void an_earlier_error() {
+  World w;
+  auto leave_error = [] { CHECK(hipFree(kSomewhere) != hipSuccess); };
+  CHECK(w.set(w.s[0], 2, 4000) == KV_OK);
+  leave_error();
+  CHECK(w.append(w.s[0]) == KV_OK);
+  leave_error();
+  CHECK(w.attn(w.s[0], true) == KV_OK);
+  leave_error();
+  launched.clear();
+  CHECK(w.evict(w.s[0], 2000) == KV_OK && launched.size() == 2);
+  mockhip::fail_after(1, hipErrorInvalidValue);  // (an injected failure: the launch's own)
+  CHECK(w.append(w.s[0]) == KV_EHIP && w.pool.last_hip == hipErrorInvalidValue);
+}
+
 }  // namespace
 
 int main(int, char** argv) {
   const std::string name = argv[1];
   if (name == "replay_then_set") replay_then_set();
   else if (name == "captures_draw_no_tickets") captures_draw_no_tickets();
+  else if (name == "an_earlier_error") an_earlier_error();
   else return 2;
   std::printf("ok\n");
   return 0;
