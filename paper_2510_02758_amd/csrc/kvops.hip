@@ -1,7 +1,8 @@
 // C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction.
-// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict, for kv_attn one
-// or two for the tiles, one for their join and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set
-// and kv_batch_destroy, and nothing is allocated there but the room for kept products and for the order of moves, when they are first needed.
+// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict (two for each
+// part of its layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
+// and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set and kv_batch_destroy, and nothing is
+// allocated there but the room for kept products and for the order of moves, when they are first needed.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -171,6 +172,9 @@ int drain(kv_batch* b) {
   if (b->used) OPCHK(b, hipStreamSynchronize(b->last));
   return KV_OK;
 }
+
+// Workgroups of 256 lanes that one launch may have: its lanes are counted in 32 bits.
+constexpr int64_t kMostWgs = (1 << 24) - 1;
 
 size_t padded(size_t bytes) { return (bytes + 63) / 64 * 64; }
 
@@ -557,6 +561,7 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
   if (pl.n == 0 || a->num_layers == 0) return KV_OK;
   if (!a->weights || !a->kept || a->weights_cap < b->max_len) return KV_EINVAL;
   const int32_t fixed_blocks = a->keep_first / v.B, keep_blocks = (int32_t)(((int64_t)a->keep + v.B - 1) / v.B);
+  if ((int64_t)pl.n * v.H * 2 > kMostWgs) return KV_EINVAL;
   const bool crowded = b->max_len > a->keep;
   if (crowded && pl.rewrites_shared(a->keep, fixed_blocks, keep_blocks)) return KV_EDUP;
   std::vector<int32_t> unchanged;
@@ -598,18 +603,18 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     k.e = v.dtype == KV_FP8_E4M3 ? 1 : 2;
     k.group = v.B >= 64 ? v.B : 64 / v.B * v.B;
     k.first_tok = fixed_blocks * v.B;
-    const unsigned heads = (unsigned)a->num_layers * pl.n * v.H;
     // chunks of the move
     constexpr int kU = 8;
     const int32_t bytes = v.D * k.e, most = bytes % 16 ? 0 : std::min(kMoveRows, kU * (256 / (bytes / 16)));
     k.rows = v.scale ? most / v.B * v.B : most;
+    const int64_t heads_layer = (int64_t)pl.n * v.H;
     bool apart = crowded && k.rows > 0;
     if (apart) {
       k.chunks = std::max(1, (a->keep - k.first_tok + k.rows - 1) / k.rows);
       if (k.chunks > 1) {
         // for any eviction of this batch
-        const size_t room = (size_t)v.L * pl.n * v.H * 2 * (2 + (size_t)b->max_len / k.rows) * 4;
-        apart = (int64_t)heads * 2 * k.chunks <= INT32_MAX && turns_room(b, room, st);
+        const size_t room = (size_t)v.L * heads_layer * 2 * (2 + (size_t)b->max_len / k.rows) * 4;
+        apart = heads_layer * 2 * k.chunks <= kMostWgs && turns_room(b, room, st);
         if (apart) k.turns = b->turns;
       }
     }
@@ -617,22 +622,32 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     // other, where there are rows enough to fill the chip with and one has the registers.  With the few moves that keeping 8 tokens needs,
     // 64 / 256 / 1024 lanes: 2048 rows of 300 to 500 tokens 25 / 35 / 131 us, 64 such 16 / 15 / 22, 160 rows of 1790 to 7026 94 / 42 / 25, 8192 of
     // 5000 to 8000 490 / 494 / 585.
-    const bool many = heads > 4u * b->v.cus;
-    auto select = [&](auto kern, int lanes) { hipLaunchKernelGGL(kern, dim3(heads), dim3(lanes), 0, st, k); };
-    if (many && b->max_len <= 64 * kSelectEach)
-      select(kv_evict_select_kernel<64>, 64);
-    else if (!many && b->max_len > 256 * kSelectEach)
-      select(kv_evict_select_kernel<1024>, 1024);
-    else
-      select(kv_evict_select_kernel<256>, 256);
-    OPCHK(b, hipGetLastError());
-    if (crowded) {
-      auto go = [&](auto kern, unsigned grid) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, k); };
-      if (apart)
-        v.scale ? go(kv_evict_move_kernel<true, kU>, heads * 2 * k.chunks) : go(kv_evict_move_kernel<false, kU>, heads * 2 * k.chunks);
+    const bool many = a->num_layers * heads_layer > 4 * v.cus;
+    // as many layers at a time as one launch may have workgroups for
+    const int32_t layers = (int32_t)std::min<int64_t>(a->num_layers, std::max<int64_t>(1, kMostWgs / (heads_layer * 2 * (apart ? k.chunks : 1))));
+    for (int32_t done = 0; done < a->num_layers; done += layers) {
+      const unsigned heads = (unsigned)(std::min(layers, a->num_layers - done) * heads_layer);
+      auto select = [&](auto kern, int lanes) { hipLaunchKernelGGL(kern, dim3(heads), dim3(lanes), 0, st, k); };
+      if (many && b->max_len <= 64 * kSelectEach)
+        select(kv_evict_select_kernel<64>, 64);
+      else if (!many && b->max_len > 256 * kSelectEach)
+        select(kv_evict_select_kernel<1024>, 1024);
       else
-        v.scale ? go(kv_evict_move_alone_kernel<true>, heads * 2) : go(kv_evict_move_alone_kernel<false>, heads * 2);
+        select(kv_evict_select_kernel<256>, 256);
       OPCHK(b, hipGetLastError());
+      if (crowded) {
+        auto go = [&](auto kern, unsigned grid) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, k); };
+        if (apart)
+          v.scale ? go(kv_evict_move_kernel<true, kU>, heads * 2 * k.chunks) : go(kv_evict_move_kernel<false, kU>, heads * 2 * k.chunks);
+        else
+          v.scale ? go(kv_evict_move_alone_kernel<true>, heads * 2) : go(kv_evict_move_alone_kernel<false>, heads * 2);
+        OPCHK(b, hipGetLastError());
+      }
+      k.w += layers * k.ws[0];
+      k.w_out += layers * k.ws[0];
+      k.kept += layers * k.ks[0];
+      k.pool += layers * k.ls;
+      if (k.scale) k.scale += layers * k.sls;
     }
   }
   if (a->req_ids) kvswap::pool_rewritten(b->pool, pl.n, a->req_ids, unchanged.data());

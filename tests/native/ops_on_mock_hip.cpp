@@ -10,7 +10,7 @@
 struct Launched {
   std::string kernel;
   dim3 grid, block;
-  const void* turns;
+  const void *turns, *pool, *kept;
   int32_t first_len;  // the batch's first length, as the launch found it in the tables when it ran (evictions)
   bool ran;
 };
@@ -26,10 +26,12 @@ void record(const char* kernel, dim3 grid, dim3 block, hipStream_t st, const Arg
 template <class Args, class... More>
 void record(const char* kernel, dim3 grid, dim3 block, hipStream_t st, const Args& a, const More&...) {
   const size_t at = launched.size();
-  launched.push_back({kernel, grid, block, nullptr, -1, false});
+  launched.push_back({kernel, grid, block, nullptr, nullptr, nullptr, -1, false});
   const int32_t* len = nullptr;
   if constexpr (std::is_same_v<Args, EvictArgs>) {
     launched[at].turns = a.turns;
+    launched[at].pool = a.pool;
+    launched[at].kept = a.kept;
     len = a.len;
   }
   mockhip::enqueue(st, [at, len] {
@@ -202,6 +204,30 @@ void an_earlier_error() {
   CHECK(w.append(w.s[0]) == KV_EHIP && w.pool.last_hip == hipErrorInvalidValue);
 }
 
+// A launch has fewer than 2^32 lanes; an eviction that needs more goes through its layers in parts, each selected and moved.
+void launches_of_a_large_eviction() {
+  World w(80, 8, 128, 16, 1 << 20);
+  const int32_t n = 512, keep = 4000;
+  CHECK(w.set(w.s[0], n, 5000) == KV_OK && w.evict(w.s[0], keep) == KV_OK);
+  const int64_t chunks = (keep + 127) / 128;  // 32 KB of rows of 256 bytes
+  int64_t moved = 0, layer = 0;
+  CHECK(launched.size() >= 4 && launched.size() % 2 == 0);
+  for (size_t i = 0; i < launched.size(); i += 2) {
+    for (size_t j = i; j < i + 2; j++) {
+      CHECK((uint64_t)launched[j].grid.x * launched[j].block.x < 1ull << 32);
+      CHECK(launched[j].pool == kSomewhere + layer * w.pool.v.ls && launched[j].kept == (const int32_t*)kSomewhere);
+    }
+    CHECK(launched[i + 1].grid.x == launched[i].grid.x * 2 * chunks && launched[i + 1].turns);
+    moved += launched[i + 1].grid.x;
+    layer += launched[i].grid.x / (n * 8);
+  }
+  CHECK(layer == 80 && moved == 80 * n * 8 * 2 * chunks);
+  // more heads than a launch can have: refused, nothing launched
+  World many(1, 1 << 15, 8, 2, 1 << 10);
+  launched.clear();
+  CHECK(many.set(many.s[0], 300, 2) == KV_OK && many.evict(many.s[0], 1) == KV_EINVAL && launched.empty());
+}
+
 }  // namespace
 
 int main(int, char** argv) {
@@ -209,6 +235,7 @@ int main(int, char** argv) {
   if (name == "replay_then_set") replay_then_set();
   else if (name == "captures_draw_no_tickets") captures_draw_no_tickets();
   else if (name == "an_earlier_error") an_earlier_error();
+  else if (name == "launches_of_a_large_eviction") launches_of_a_large_eviction();
   else return 2;
   std::printf("ok\n");
   return 0;
