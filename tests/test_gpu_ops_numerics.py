@@ -1,0 +1,52 @@
+"""Where the attention's 16-bit arithmetic can go wrong, on a real MI355X: weights and scales far apart, and values that are not finite.
+Against the definition in 64 bits."""
+import numpy as np
+import pytest
+
+import ops_ref as R
+from paper_2510_02758_amd import kvswap as kv
+from paper_2510_02758_amd import workloads as W
+from test_gpu_ops import Pool, _tables, _torch_type
+
+pytestmark = pytest.mark.gpu
+
+
+def _attend(p, rows, lens, q_lens, q, scale):
+    import torch
+    o, ids = R.csr(rows)
+    out = torch.empty_like(q)
+    kv.kv_check(p.batch.set(o, ids, lens, q_lens, q.shape[1]))
+    kv.kv_check(p.batch.attn(0, q, out, scale))
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("drop", [8, 12, 14, 16, 18, 20])
+@pytest.mark.parametrize("G", [4, 32])  # row tiles, big tiles
+@pytest.mark.parametrize("B", [16, 5])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "fp8_e4m3"])
+def test_many_small_weights_beside_a_large_one(gpu, dtype, B, G, drop):
+    """One key that takes most of the weight and has no value, before many alike that lie `drop` below it: the output is what these have in
+    all.  Scores are exact here; a weight is rounded once to 16 bits, and to no less than 2^-34 of the largest (f16), the output once."""
+    import torch
+    n, D = 20000, 64
+    N = -(-n // B) + 2
+    p = Pool(gpu, W.Geometry(1, 1, D, B, dtype, N), seed=1)
+    rows = _tables(p.rng, N, [n], B)
+    x = np.arange(n)
+    at = (torch.from_numpy(rows[0].astype(np.int64)[x // B]).to(gpu), torch.from_numpy(x % B).to(gpu))
+    values = torch.zeros(2, N, B, 1, D, device=gpu)
+    values[0, at[0], at[1], 0, 0] = -float(drop)
+    values[1, at[0], at[1]] = 1.0
+    values[:, at[0][0], at[1][0]] = 0.0
+    stored = values.to(_torch_type(dtype))
+    p.bits()[0] = stored.view(torch.uint8 if dtype == "fp8_e4m3" else torch.int16)
+    for io_name in ([dtype] if dtype != "fp8_e4m3" else ["bf16", "f16"]):
+        q = torch.zeros(1, G, D, device=gpu, dtype=_torch_type(io_name))
+        q[:, :, 0] = 1.0
+        got = _attend(p, rows, [n], [1], q, 1.0)
+        tail = (n - 1) * np.exp(-float(drop))
+        want = tail / (1 + tail)
+        u = R.U[io_name]
+        tol = want * (2 * u + 2.0 ** -14) + ((n * 2.0 ** -34 + 2.0 ** -25) if io_name == "f16" else 0)
+        assert (np.abs(got - want) <= tol).all(), (io_name, want, np.abs(got - want).max())
