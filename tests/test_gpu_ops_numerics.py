@@ -50,3 +50,44 @@ def test_many_small_weights_beside_a_large_one(gpu, dtype, B, G, drop):
         u = R.U[io_name]
         tol = want * (2 * u + 2.0 ** -14) + ((n * 2.0 ** -34 + 2.0 ** -25) if io_name == "f16" else 0)
         assert (np.abs(got - want) <= tol).all(), (io_name, want, np.abs(got - want).max())
+
+
+@pytest.mark.parametrize("io_name", ["f16", "bf16"])
+@pytest.mark.parametrize("B", [16, 6])
+@pytest.mark.parametrize("new,G", [(1, 4), (1, 32), (3, 4), (40, 4)])  # row tiles, big tiles; without and with tokens that some rows do not see
+@pytest.mark.parametrize("D", [64, 72])
+def test_value_scales_far_apart(gpu, D, new, G, B, io_name):
+    """Blocks whose values have large scales, but which get little weight, or which a row does not see at all: neither takes the precision of the
+    others away."""
+    import torch
+    n, light = 300, 200
+    N = -(-n // B) + 2
+    p = Pool(gpu, W.Geometry(1, 2, D, B, "fp8_e4m3", N, scales=True), seed=2)
+    rows = _tables(p.rng, N, [n], B)
+    p.fill(rows, [n])
+    x = np.arange(n)
+    blk, place = rows[0].astype(np.int64)[x // B], x % B
+    values = torch.randn(2, N, B, 2, D, generator=torch.Generator().manual_seed(3)).clamp_(-4, 4)
+    values[0] = 0.0
+    light_at = (torch.from_numpy(blk[light:]), torch.from_numpy(place[light:]))
+    values[0, light_at[0], light_at[1], :, 0] = -18.0  # a score of -18 beside 0
+    used = torch.zeros(N, B, dtype=torch.bool)
+    used[torch.from_numpy(blk), torch.from_numpy(place)] = True
+    bits = values.to(torch.float8_e4m3fn).view(torch.uint8)
+    bits[:, ~used] = 0x7F
+    p.bits()[0] = bits.to(gpu)
+    p.scale[0, 0] = 1.0
+    p.scale[0, 1] = 1e-3
+    # blocks of light tokens only that every row sees have large scales; the last block, which the last row alone sees whole, a huge one
+    whole = [b for b in range(-(-light // B), (n - new) // B)]
+    p.scale[0, 1, torch.from_numpy(rows[0].astype(np.int64)[whole]).to(gpu)] = 1e7
+    last = (n - 1) // B
+    first_row_of_last = max(0, last * B - (n - new))  # rows that see some of it
+    if first_row_of_last:
+        p.scale[0, 1, int(rows[0][last])] = 1e25
+    q = torch.zeros(new, 2 * G, D, dtype=_torch_type(io_name), device=gpu)
+    q[:, :, 0] = 1.0
+    got = _attend(p, rows, [n], [new], q, 1.0)
+    ref, tol, _, _, _, _ = R.attention(p.values()[0], rows, [n], [new], q.double().cpu().numpy(), 1.0, io_name, B)
+    seen = first_row_of_last or new
+    assert (np.abs(got - ref)[:seen] <= tol[:seen] + 2.0 ** -25).all(), (np.abs(got - ref) / tol)[:seen].max()
