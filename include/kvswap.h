@@ -502,7 +502,10 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream);
  * that sees nothing has out 0 and lse -inf.  What lies in a block behind a request's last token is never used, whatever it holds.
  * weights (nullable) [n][H][weights_cap]: weights[i][h][x] += the softmax weights of cached token x of request i, over the request's rows
  * and the query heads of h; places from num_tokens[i] on stay as they are.
- * Arithmetic: products of io-type elements (fp8 ones widened exactly) accumulate in 32 bits; softmax and sums in 32 bits. */
+ * Arithmetic: products of io-type elements (fp8 ones widened exactly) accumulate in 32 bits; softmax statistics and sums are 32 bits; out is
+ * rounded once.  For the product with V the weights go into 16 bits: in two terms, which leave out less than 2^-16 of each (in f16: or 2^-34 of
+ * the row's largest), or in one, rounded to io_dtype as out is.  One term is for the tokens that a request has for itself where it has more than
+ * 16 rows for a KV head (new tokens times query heads: a prompt); all else has two, whatever other requests are in the batch. */
 typedef struct {
   uint32_t struct_size;
   int32_t layer;

@@ -27,7 +27,8 @@ struct AttnItem {
   int32_t row0, rows;
   int32_t part;     // partial row of row0; -1: the rows are finished here
   // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
-  int32_t score, score_row, score_from, pad;
+  int32_t score, score_row, score_from;
+  int32_t fine;  // big tiles: keys that several requests share.  Their weights are as precise as in row tiles, whatever these requests' number
 };
 // One piece of weight accumulation whose products are computed again: keys [k0, k1) that `count` requests have in common, for the
 // rows of these, requests wreqs[first ..].
@@ -366,7 +367,7 @@ class BatchPlan {
   void add(const Tile& t, int32_t k0, int32_t k1, int32_t part, bool* any_mixed) {
     const int32_t end = std::max(k0, std::min(k1, t.limit));
     items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part,
-                     t.score, t.score_row, nodes_[t.node].from, 0});
+                     t.score, t.score_row, nodes_[t.node].from, nodes_[t.node].reqs.size() > 1});
     if (items.back().clear < end) *any_mixed = true;
   }
   int32_t take_rows(const Tile& t, int32_t rows) {

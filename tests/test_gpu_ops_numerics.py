@@ -91,3 +91,31 @@ def test_value_scales_far_apart(gpu, D, new, G, B, io_name):
     ref, tol, _, _, _, _ = R.attention(p.values()[0], rows, [n], [new], q.double().cpu().numpy(), 1.0, io_name, B)
     seen = first_row_of_last or new
     assert (np.abs(got - ref)[:seen] <= tol[:seen] + 2.0 ** -25).all(), (np.abs(got - ref) / tol)[:seen].max()
+
+
+@pytest.mark.parametrize("n", [8, 17, 150])  # row tiles, one big tile, several
+@pytest.mark.parametrize("B,D", [(16, 64), (16, 128), (16, 256), (6, 72)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8_e4m3"])
+def test_rows_behind_a_prefix_are_as_precise_whatever_their_number(gpu, dtype, B, D, n):
+    """Two tokens of a shared prefix with values 1 and -1 and scores 0 and -a, all others without weight: the output is tanh(a/2), a difference of
+    weights.  These carry 16 bits and more (2^-16 of their sum), and the output is rounded once."""
+    import torch
+    shared, lens = 13, [13 * B + 1] * n
+    N = shared + n + 2
+    p = Pool(gpu, W.Geometry(1, 1, D, B, dtype, N), seed=4)
+    perm = p.rng.permutation(N).astype(np.int32)
+    rows = [np.concatenate([perm[:shared], perm[shared + i:shared + i + 1]]) for i in range(n)]
+    values = torch.zeros(2, N, B, 1, D)
+    values[0, ..., 0] = -64.0
+    values[0, int(perm[0]), 0, 0, 0], values[0, int(perm[0]), 1, 0, 0] = 0.0, -1.0
+    values[1, int(perm[0]), 0], values[1, int(perm[0]), 1] = 1.0, -1.0
+    p.bits()[0] = values.to(_torch_type(dtype)).view(torch.uint8 if dtype == "fp8_e4m3" else torch.int16).to(gpu)
+    for io_name in ([dtype] if dtype != "fp8_e4m3" else ["bf16", "f16"]):
+        q = torch.zeros(n, 1, D)
+        a = torch.linspace(0.3, 1.5, n).to(_torch_type(io_name))
+        q[:, 0, 0] = a.float()
+        q = q.to(gpu, _torch_type(io_name))
+        got = _attend(p, rows, lens, [1] * n, q, 1.0)
+        want = np.tanh(a.double().numpy() / 2)[:, None, None]
+        tol = R.U[io_name] * want * (1 + 2.0 ** -7) + 2.0 ** -16
+        assert (np.abs(got - want) <= tol).all(), (io_name, (np.abs(got - want) / tol).max())
