@@ -500,6 +500,8 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream);
 /* out[t][hq] = sum over the cached tokens x that row t sees of softmax(scale * q[t][hq] . K[x])[x] * V[x]; new token j of a request
  * sees its request's tokens up to its own index.  lse[t][hq] (nullable) is the logarithm of the softmax's sum.  A row
  * that sees nothing has out 0 and lse -inf.  What lies in a block behind a request's last token is never used, whatever it holds.
+ * An infinity among the values that a row sees makes that element of its out infinite, two of unlike sign or a NaN make it a NaN (and so does
+ * an infinity whose weight 32 bits do not tell from none beside the other keys').
  * weights (nullable) [n][H][weights_cap]: weights[i][h][x] += the softmax weights of cached token x of request i, over the request's rows
  * and the query heads of h; places from num_tokens[i] on stay as they are.
  * Arithmetic: products of io-type elements (fp8 ones widened exactly) accumulate in 32 bits; softmax statistics and sums are 32 bits; out is

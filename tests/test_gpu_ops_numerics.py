@@ -119,3 +119,52 @@ def test_rows_behind_a_prefix_are_as_precise_whatever_their_number(gpu, dtype, B
         want = np.tanh(a.double().numpy() / 2)[:, None, None]
         tol = R.U[io_name] * want * (1 + 2.0 ** -7) + 2.0 ** -16
         assert (np.abs(got - want) <= tol).all(), (io_name, (np.abs(got - want) / tol).max())
+
+
+ODD = {
+    # H, D, B, G, lens, q_lens, requests that share their first blocks
+    "decode": (2, 128, 16, 4, [300, 70], [1, 1], ()),
+    "decode, d 72": (2, 72, 6, 4, [300, 70], [1, 1], ()),
+    "decode, d 256": (1, 256, 16, 4, [300, 70], [1, 1], ()),
+    "decode, cut": (1, 64, 16, 4, [9000, 70], [1, 1], ()),
+    "two new tokens": (2, 128, 16, 4, [300, 70], [2, 2], ()),
+    "two new tokens, d 256": (1, 256, 16, 4, [300, 70], [2, 2], ()),
+    "many heads": (1, 128, 16, 40, [300, 70], [1, 1], ()),
+    "prompt": (2, 128, 16, 4, [300, 70], [180, 40], ()),
+    "prompt, d 72": (2, 72, 6, 4, [300, 70], [180, 40], ()),
+    "prompt, d 256": (1, 256, 16, 4, [300, 70], [180, 40], ()),
+    "prefix": (2, 64, 16, 4, [300 + i for i in range(9)], [1] * 9, tuple((i, 0, 17) for i in range(1, 9))),
+    "prefix, d 96": (1, 96, 5, 4, [300 + i for i in range(9)], [1] * 9, tuple((i, 0, 55) for i in range(1, 9))),
+}
+
+
+@pytest.mark.parametrize("name", list(ODD))
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_infinities_among_the_values(gpu, dtype, name):
+    """An infinity in a value makes that element of the rows that see it infinite, two of unlike sign or a NaN make it a NaN; other elements, and
+    rows that do not see the token, are as without."""
+    import torch
+    H, D, B, G, lens, q_lens, shared = ODD[name]
+    N = sum(-(-n // B) for n in lens) + 3
+    p = Pool(gpu, W.Geometry(1, H, D, B, dtype, N), seed=7)
+    rows = _tables(p.rng, N, lens, B, shared)
+    p.fill(rows, lens)
+    q = torch.from_numpy(p.rng.standard_normal((sum(q_lens), H * G, D))).to(_torch_type(dtype)).to(gpu)
+    clean, tol, _, _, _, _ = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), D ** -0.5, dtype, B)
+    up, nan = {"bf16": (0x7F80, 0x7FC0), "f16": (0x7C00, 0x7E00)}[dtype]
+    down = up - 0x8000  # (as a signed word)
+    first, last, new = 5, lens[0] - 2, lens[0] - max(2, q_lens[0] // 2)
+    #       token, element, bits; element 0: one infinity, 1: one below zero, 2: both, 3: twice the same, 4: NaN, 5 and 6: seen by later rows only
+    odd = [(first, 0, up), (first, 1, down), (first, 2, up), (33, 2, down), (first, 3, up), (34, 3, up), (40, 4, nan), (last, 5, up), (last, 6, down),
+           (new, 6, up), (new, D - 1, down)]
+    for token, d, bits in odd:
+        p.bits()[0, 1, int(rows[0][token // B]), token % B, :, d] = bits
+    with np.errstate(invalid="ignore"):
+        want, _, _, _, _, _ = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), D ** -0.5, dtype, B)
+    got = _attend(p, rows, lens, q_lens, q, D ** -0.5)
+    assert np.isposinf(want).any() and np.isneginf(want).any() and np.isnan(want).any()
+    assert np.array_equal(np.isposinf(got), np.isposinf(want))
+    assert np.array_equal(np.isneginf(got), np.isneginf(want))
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    fine = np.isfinite(want)
+    assert (np.abs(got - clean)[fine] <= tol[fine]).all()
