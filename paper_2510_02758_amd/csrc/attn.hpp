@@ -6,6 +6,8 @@
 
 #include "batch.hpp"
 
+using kvswap::big_tile;
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -103,6 +105,3 @@ template <typename E>
 void launch_join(const JoinArgs& j, const kvswap::BatchPlan& pl, hipStream_t st);
 template <typename E>
 void launch_weights(bool fp8, const WeightArgs& w, int items, hipStream_t st);
-
-// Rows of a big tile: what a wavefront's registers hold of their outputs.
-constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }

@@ -278,16 +278,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     pl.n = pl.T = 0;
     return rc;
   }
-  kvswap::BatchShape shape;
-  shape.H = b->v.H;
-  shape.B = b->v.B;
-  shape.N = b->v.N;
-  // Two workgroups of row tiles a CU: with three, more places of the pool are read at a time, and each more slowly (64 requests of 512 to
-  // 4096 tokens on 8 heads of 128 in bf16: 103 us with two, 122 with three, 140 with one; 32 of 256 to 8192 on 32 heads in fp8: 181, 185, 242).
-  shape.wgs = b->v.cus * 2;
-  shape.big_wgs = b->v.cus * (b->v.D <= 128 ? 2 : 1);
-  shape.big_tile = big_tile(b->v.D);
-  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, shape);
+  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus));
   if (rc) return rc;
   b->max_len = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);
