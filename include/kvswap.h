@@ -427,10 +427,11 @@ typedef struct kv_batch kv_batch; /* opaque */
 
 /* A batch on the pool; the pool must outlive it (KV_EINVAL: a head_dim that is no multiple of 8, above 128 none of 16, or above 256).
  * The batch owns device memory for the tables, the plan of the attention and its partial results, which kv_batch_set allocates as
- * batches grow, and from the first kv_attn with weights on for products, which grows then with the batches (4 bytes for each of a
- * row tile's up to 16 rows and its keys; a call in a capture takes none and computes products twice instead).  So does kv_evict for
- * the order of its moves (8 bytes for each layer, head and some 128 tokens of the longest request, times n; in a capture each head's
- * moves are always made one after the other instead). */
+ * batches grow (it waits on the host for the batch's earlier work where it does).  Two more parts are allocated by the first call that wants them, and
+ * from then on by kv_batch_set.  One is kv_attn's with weights, for products: 4 bytes for each of a row tile's up to 16 rows and its keys.  Without
+ * it, for want of memory or because the first such call is in a capture, they are computed twice.  The other is kv_evict's, for the order of its moves:
+ * 8 bytes for each layer, head and some 128 tokens of the longest request, times n.  Without it, and always in a capture, each head's moves are made
+ * one after the other. */
 int kv_batch_create(kv_pool* p, kv_batch** out);
 /* Waits for the batch's work (for the device, if calls have been captured since the batch was set), then frees it. */
 int kv_batch_destroy(kv_batch* b);

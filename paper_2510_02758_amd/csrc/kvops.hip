@@ -2,7 +2,7 @@
 // Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict (two for each
 // part of its layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
 // and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set and kv_batch_destroy, and nothing is
-// allocated there but the room for kept products and for the order of moves, when they are first needed.
+// allocated there but the first room for kept products and for the order of moves, when they are first needed.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -52,13 +52,13 @@ struct kv_batch {
   float *part_o = nullptr, *lse = nullptr;
   float2* part_ml = nullptr;
 
-  // Products of row tiles that the weights are computed from, taken when weights are first asked for (and not in a capture).
-  float* scores = nullptr;
-  size_t scores_cap = 0;
-
-  // Tickets of an eviction's chunks, taken when an eviction first needs them; none in a capture.
-  int32_t* turns = nullptr;
-  size_t turns_cap = 0;
+  // Products of row tiles that the weights are computed from, and tickets of an eviction's chunks.  The first call that wants one of them takes it
+  // (not in a capture); from then on kv_batch_set sees to it that there is room for its batch.
+  struct Room {
+    char* at = nullptr;
+    size_t cap = 0;
+    bool wanted = false;
+  } scores, turns;
 
   // The stream of the newest work; another stream's call waits for what is on it.
   bool used = false;
@@ -105,42 +105,46 @@ struct Relaxed {
   }
 };
 
-// Room for the batch's kept products; false: there is none, they have to be computed again.
-bool scores_room(kv_batch* b, hipStream_t st) {
-  const size_t need = (size_t)b->plan.scores * b->v.H * 4;
-  if (need <= b->scores_cap) return true;
-  if (is_capturing(st)) return false;
-  if (b->scores) {  // earlier calls may still use it; hipFree waits for them
-    (void)hipFree(b->scores);
-    b->scores = nullptr;
-    b->scores_cap = 0;
-  }
-  if (hipMalloc((void**)&b->scores, need + need / 4) != hipSuccess) {
+// Room of `need` bytes that nobody uses; none if there is not that much memory.
+void take(kv_batch::Room& r, size_t need) {
+  if (hipMalloc((void**)&r.at, need + need / 4) == hipSuccess) {
+    r.cap = need + need / 4;
+  } else {
     (void)hipGetLastError();
-    b->scores = nullptr;
-    return false;
+    r.at = nullptr;
   }
-  b->scores_cap = need + need / 4;
-  return true;
 }
 
-// Room for the tickets of an eviction's chunks.  None in a capture: two launches that drew from the same tickets at a time would leave
-// chunks out and wait for these, and when a replay runs is not known here.
-bool turns_room(kv_batch* b, size_t need, hipStream_t st) {
-  if (is_capturing(st)) return false;
-  if (need <= b->turns_cap) return true;
-  if (b->turns) {
-    (void)hipFree(b->turns);
-    b->turns = nullptr;
-    b->turns_cap = 0;
-  }
-  if (hipMalloc((void**)&b->turns, need + need / 4) != hipSuccess) {
-    (void)hipGetLastError();
-    b->turns = nullptr;
+// In a call: is there room?  Only the first call of all may take some: kv_batch_set has grown what has been wanted before as far as it could.
+bool has_room(kv_batch::Room& r, size_t need, hipStream_t st) {
+  const bool first = !r.wanted;
+  r.wanted = true;
+  if (need <= r.cap) return true;
+  if (is_capturing(st)) {
+    r.wanted = !first || r.at;  // (the next call that is not captured is the first)
     return false;
   }
-  b->turns_cap = need + need / 4;
-  return true;
+  if (!first) return false;
+  Relaxed relaxed;
+  take(r, need);
+  return need <= r.cap;
+}
+
+// Room for the batch's kept products.
+size_t scores_need(const kv_batch* b) { return (size_t)b->plan.scores * b->v.H * 4; }
+
+// Bytes of an element of the pool, and rows of a chunk of an eviction's moves (0: moves are not made in chunks).
+int32_t elem(const PoolView& v) { return v.dtype == KV_FP8_E4M3 ? 1 : 2; }
+constexpr int kMoveUnroll = 8;
+int32_t chunk_rows(const PoolView& v) {
+  const int32_t bytes = v.D * elem(v), most = bytes % 16 ? 0 : std::min(kMoveRows, kMoveUnroll * (256 / (bytes / 16)));
+  return v.has_scale ? most / v.B * v.B : most;
+}
+
+// Room for the tickets of any eviction of this batch.
+size_t turns_need(const kv_batch* b) {
+  const int32_t rows = chunk_rows(b->v);
+  return rows ? (size_t)b->v.L * b->plan.n * b->v.H * 2 * (2 + (size_t)b->max_len / rows) * 4 : 0;
 }
 
 // Puts `st` behind the batch's work on another stream.  The checks behind the launches read the thread's last HIP error, which any earlier
@@ -162,7 +166,6 @@ int order(kv_batch* b, hipStream_t st) {
 // Waits for replays of captured calls, which may be on any stream, before what they read is changed or freed.
 int settle(kv_batch* b) {
   if (!b->captured) return KV_OK;
-  Relaxed relaxed;
   OPCHK(b, hipDeviceSynchronize());
   b->captured = false;
   return KV_OK;
@@ -188,7 +191,7 @@ DivBy division(int32_t B) {
 KvSide side(const kv_batch* b, int32_t layer) {
   const PoolView& v = b->v;
   KvSide s{};
-  const int e = v.dtype == KV_FP8_E4M3 ? 1 : 2;
+  const int e = elem(v);
   s.k = v.pool + layer * v.ls;
   s.vk = v.ks;
   s.bs = v.bs;
@@ -255,8 +258,8 @@ int kv_batch_destroy(kv_batch* b) try {
       if (u) (void)hipHostFree(u);
     if (b->mem) (void)hipFree(b->mem);
     if (b->ws) (void)hipFree(b->ws);
-    if (b->scores) (void)hipFree(b->scores);
-    if (b->turns) (void)hipFree(b->turns);
+    if (b->scores.at) (void)hipFree(b->scores.at);
+    if (b->turns.at) (void)hipFree(b->turns.at);
   }
   delete b;
   return rc;
@@ -273,6 +276,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
   hipStream_t st = (hipStream_t)stream;
   if (!b->v.plan_only && (is_capturing(st) || (b->used && b->last != st && is_capturing(b->last)))) return KV_EINVAL;
   BatchPlan& pl = b->plan;
+  Relaxed relaxed;
   rc = settle(b);
   if (rc) {
     pl.n = pl.T = 0;
@@ -327,6 +331,15 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     OPCHK(b, hipMalloc((void**)&b->ws, ws_need + ws_need / 2));
     b->ws_cap = ws_need + ws_need / 2;
   }
+  const std::pair<kv_batch::Room*, size_t> rooms[2] = {{&b->scores, scores_need(b)}, {&b->turns, turns_need(b)}};
+  for (auto [room, room_need] : rooms)
+    if (room->wanted && room_need > room->cap) {
+      rc = drain(b);
+      if (rc) return rc;
+      if (room->at) OPCHK(b, hipFree(room->at));
+      *room = {nullptr, 0, true};
+      take(*room, room_need);
+    }
   if (b->up_busy[k]) OPCHK(b, hipEventSynchronize(b->up_ev[k]));
   b->up_busy[k] = false;
   if (need > b->up_cap[k]) {
@@ -510,9 +523,9 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
   k.hw = pl.heads;
   k.q_vec = aligned(a->q, a->q_strides, 16);
   k.o_vec = aligned(a->out, a->out_strides, 8);
-  const bool keeps = a->weights && pl.scores && scores_room(b, st);
+  const bool keeps = a->weights && pl.scores && has_room(b->scores, scores_need(b), st);
   if (keeps) {
-    k.scores = b->scores;
+    k.scores = (float*)b->scores.at;
     k.scores_head = pl.scores;
   }
   const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16;
@@ -591,22 +604,21 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
     k.sbs = v.sbs;
     k.D = v.D;
     k.B = v.B;
-    k.e = v.dtype == KV_FP8_E4M3 ? 1 : 2;
+    k.e = elem(v);
     k.group = v.B >= 64 ? v.B : 64 / v.B * v.B;
     k.first_tok = fixed_blocks * v.B;
     // chunks of the move
-    constexpr int kU = 8;
-    const int32_t bytes = v.D * k.e, most = bytes % 16 ? 0 : std::min(kMoveRows, kU * (256 / (bytes / 16)));
-    k.rows = v.scale ? most / v.B * v.B : most;
+    constexpr int kU = kMoveUnroll;
+    k.rows = chunk_rows(v);
     const int64_t heads_layer = (int64_t)pl.n * v.H;
     bool apart = crowded && k.rows > 0;
     if (apart) {
       k.chunks = std::max(1, (a->keep - k.first_tok + k.rows - 1) / k.rows);
       if (k.chunks > 1) {
-        // for any eviction of this batch
-        const size_t room = (size_t)v.L * heads_layer * 2 * (2 + (size_t)b->max_len / k.rows) * 4;
-        apart = heads_layer * 2 * k.chunks <= kMostWgs && turns_room(b, room, st);
-        if (apart) k.turns = b->turns;
+        // No tickets in a capture: two launches that drew from the same ones at a time would leave chunks out and wait for these, and when a
+        // replay runs is not known here.
+        apart = heads_layer * 2 * k.chunks <= kMostWgs && !is_capturing(st) && has_room(b->turns, turns_need(b), st);
+        if (apart) k.turns = (int32_t*)b->turns.at;
       }
     }
     // Lanes of a row's workgroup: 256; more where a few rows are longer than these have registers for; a wavefront, which waits for no

@@ -204,6 +204,31 @@ void an_earlier_error() {
   CHECK(w.append(w.s[0]) == KV_EHIP && w.pool.last_hip == hipErrorInvalidValue);
 }
 
+// Calls allocate nothing but the first room that one of them wants, free nothing, and do not wait: kv_batch_set grows what has been wanted.
+void room_is_grown_by_set() {
+  World w;
+  auto calls = [&] { return mockhip::resource_calls(); };
+  CHECK(w.set(w.s[0], 2, 300) == KV_OK);
+  const long waits = mockhip::host_waits();
+  long before = calls();
+  CHECK(w.attn(w.s[0], true) == KV_OK && calls() == before + 1);
+  CHECK(w.evict(w.s[0], 140) == KV_OK && launched.back().turns && calls() == before + 2);
+  CHECK(w.attn(w.s[0], true) == KV_OK && w.evict(w.s[0], 140) == KV_OK && calls() == before + 2 && mockhip::host_waits() == waits);
+  CHECK(w.set(w.s[0], 9, 9000) == KV_OK);
+  const long waits_then = mockhip::host_waits();
+  before = calls();
+  CHECK(w.attn(w.s[0], true) == KV_OK && w.evict(w.s[0], 5000) == KV_OK && launched.back().turns);
+  CHECK(calls() == before && mockhip::host_waits() == waits_then);
+  // a first call in a capture takes nothing; the first one outside does
+  World other;
+  CHECK(other.set(other.s[0], 2, 300) == KV_OK);
+  before = calls();
+  mockhip::begin_capture(other.s[0]);
+  CHECK(other.attn(other.s[0], true) == KV_OK && other.evict(other.s[0], 140) == KV_OK && calls() == before);
+  mockhip::end_capture();
+  CHECK(other.attn(other.s[0], true) == KV_OK && other.evict(other.s[0], 140) == KV_OK && calls() == before + 2);
+}
+
 // A launch has fewer than 2^32 lanes; an eviction that needs more goes through its layers in parts, each selected and moved.
 void launches_of_a_large_eviction() {
   World w(80, 8, 128, 16, 1 << 20);
@@ -236,6 +261,7 @@ int main(int, char** argv) {
   else if (name == "captures_draw_no_tickets") captures_draw_no_tickets();
   else if (name == "an_earlier_error") an_earlier_error();
   else if (name == "launches_of_a_large_eviction") launches_of_a_large_eviction();
+  else if (name == "room_is_grown_by_set") room_is_grown_by_set();
   else return 2;
   std::printf("ok\n");
   return 0;
