@@ -253,6 +253,28 @@ void launches_of_a_large_eviction() {
   CHECK(many.set(many.s[0], 300, 2) == KV_OK && many.evict(many.s[0], 1) == KV_EINVAL && launched.empty());
 }
 
+// The kernels' angles of far positions: products that wrap around are taken without a sign (run under the sanitizer; no lane sees another's).
+void far_positions() {
+  uint16_t k[8] = {}, v[8] = {}, pool[2 * 8] = {};
+  const int64_t turns[4] = {(int64_t)1 << 61, 123456789012345678, -1, INT64_MIN};
+  for (const int32_t pos : {2000000000, -2000000000, INT32_MIN, 0}) {
+    const kvswap::TokenPlace place{0, 0, pos, 0};
+    AppendArgs a{};
+    a.k = (const char*)k;
+    a.v = (const char*)v;
+    a.turns = turns;
+    a.positions = pos ? &pos : nullptr;
+    a.places = &place;
+    a.pool = (char*)pool;
+    a.vk = sizeof(pool) / 2;
+    a.magnitude = 1;
+    a.rot = a.D = 8;
+    a.H = a.chunks = a.pairs = a.units = a.interleaved = 1;
+    mockhip::run_grid(dim3(1), dim3(256), 0, [&] { kv_append_kernel<__bf16, false>(a); });
+    mockhip::run_grid(dim3(1), dim3(256), 0, [&] { kv_append_wide_kernel<__bf16, false>(a); });
+  }
+}
+
 }  // namespace
 
 int main(int, char** argv) {
@@ -262,6 +284,7 @@ int main(int, char** argv) {
   else if (name == "an_earlier_error") an_earlier_error();
   else if (name == "launches_of_a_large_eviction") launches_of_a_large_eviction();
   else if (name == "room_is_grown_by_set") room_is_grown_by_set();
+  else if (name == "far_positions") far_positions();
   else return 2;
   std::printf("ok\n");
   return 0;
