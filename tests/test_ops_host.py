@@ -28,3 +28,11 @@ def test_host_side(ops, name):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:detect_stack_use_after_return=0")
     r = subprocess.run([ops, name], capture_output=True, text=True, timeout=120, env=env)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_which_evictions_reach_shared_blocks(tmp_path):
+    exe = str(tmp_path / "rewrites_shared")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-Wall", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                           os.path.join(HERE, "native", "rewrites_shared.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "checks ok" in r.stdout, r.stdout + r.stderr
