@@ -477,8 +477,8 @@ int kv_rope_freqs(int32_t rot, double base, int32_t kind, double factor, double 
  * pair j, (2j, 2j+1) if interleaved, else (j, j + rot/2), by positions[t] * turns[j] (positions NULL: the cache index; an evicted
  * cache's positions run ahead of its indices).  The turned q goes to q_out (may be q; neither is used if q is NULL), the turned
  * k and v into the pool: rounded once from 32 bits.  An fp8 pool takes value / scale[h], beyond +-448 as +-448; with scales,
- * k_scale and v_scale [H] are stored as the scales of every block that a token goes to: a block's tokens must all have been
- * stored with the same ones.  Without scales in the pool both are NULL.
+ * k_scale and v_scale [H] are stored as the scales of every block that a token goes to, and what the block's other tokens stand for goes with
+ * them: a block's tokens must all have been stored with the same ones (see kv_evict).  Without scales in the pool both are NULL.
  * Two rows must not have the same place in the pool: requests only append to blocks that they do not share. */
 typedef struct {
   uint32_t struct_size;
@@ -531,7 +531,9 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream);
  * indices that they leave have weight 0.  kept[layer][i][h][0 .. min(keep, num_tokens[i]) - 1] are their former indices.  Requests
  * with at most `keep` tokens stay (their weights are copied).  Afterwards a request has min(keep, num_tokens[i]) tokens, and the blocks behind
  * these are free; the batch still describes it as before, so set it again.  In a pool with scales a block takes the
- * largest scale that its tokens come with, and tokens that come with less are rounded to it.
+ * largest scale that its tokens come with, and tokens that come with less are rounded to it.  Where a pool's blocks differ in their scales, keep
+ * has to be a multiple of B: then the next token begins a block, and kv_append gives that one its scales.  With another keep it goes to the last
+ * block that stays, whose scales kv_append would replace.
  * weights [num_layers][n][H][weights_cap]; weights_out the same (NULL or the same pointer: in place).
  * req_ids (host, nullable) [n]: requests that the staging arena may hold copies of; their watermark and staged blocks go back to the
  * blocks that have not changed, and they leave the write queue.

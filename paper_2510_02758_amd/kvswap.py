@@ -748,7 +748,8 @@ class KVBatch:
 
     def evict(self, layer, num_layers, weights, kept, keep, keep_first=0, keep_last=0, weights_out=None, req_ids=None, stream=None):
         """weights, weights_out (default: weights itself): float32 [num_layers, n, H, cap] of the same strides; kept: int32
-        [num_layers, n, H, keep or more]; req_ids: host uint64 [n]."""
+        [num_layers, n, H, keep or more]; req_ids: host uint64 [n].  In a pool with scales that differ from block to block keep has to be a
+        multiple of the block size, so that the next append begins a block."""
         if not self.h or not self.pool.h or weights.dim() != 4 or kept.dim() != 4 or kept.shape[3] < min(keep, self.max_len):
             return KV_EINVAL
         lead, ws, ks, out, ids = (num_layers, self.n, self.geom.H), weights.stride(), kept.stride(), 0, 0
