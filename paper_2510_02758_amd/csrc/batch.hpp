@@ -53,6 +53,8 @@ struct BatchShape {
   int big_wgs = 512;    // the same two for big tiles
   int big_least = 512;
   int big_tile = 128;   // rows of a big tile
+  int big_cu = 2;       // workgroups of big tiles that share a CU
+  int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
 };
 
 // Rows of a big tile: what a wavefront's registers hold of their outputs.
@@ -61,13 +63,15 @@ constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }
 // What a pool's batches are laid out for on a GPU of `cus` compute units.  Two workgroups of row tiles a CU: with three, more places of the pool are
 // read at a time, and each more slowly (64 requests of 512 to 4096 tokens on 8 heads of 128 in bf16: 103 us with two, 122 with three, 140 with
 // one; 32 of 256 to 8192 on 32 heads in fp8: 181, 185, 242).
-inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus) {
+inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus, bool fp8) {
   BatchShape s;
   s.H = H;
   s.B = B;
   s.N = N;
   s.wgs = cus * 2;
-  s.big_wgs = cus * (D <= 128 ? 2 : 1);
+  s.big_cu = D <= 128 ? 2 : 1;
+  s.big_wgs = cus * s.big_cu;
+  s.key_rows = fp8 ? 100 : 50;
   s.big_tile = big_tile(D);
   return s;
 }
@@ -279,6 +283,8 @@ class BatchPlan {
     int32_t list, tokens, part;  // every row of these tokens has a partial row from here on
   };
   std::vector<Tile> few_, big_, huge_;
+  int big_cu_ = 1;
+  double row_cost_ = 0;  // keys that the partial rows of a big tile's piece cost
   std::vector<int32_t> seen_;  // nodes with keys, per token
   std::vector<Use> uses_;
 
@@ -301,6 +307,8 @@ class BatchPlan {
     // Tiles have whole tokens, so that a token's rows are together wherever a tile's keys are cut; where one token has more rows than a
     // big tile, its tiles are cut alike instead.
     const int32_t big_tokens = s.big_tile / G;
+    big_cu_ = s.big_cu;
+    row_cost_ = (double)s.big_tile * s.H / s.key_rows;
     for (size_t d = 0; d < nodes_.size(); d++) {
       const Node& node = nodes_[d];
       const int32_t list = (int32_t)lists.size();
@@ -404,23 +412,52 @@ class BatchPlan {
     return part;
   }
 
+  int64_t keys_of(const Tile& t) const { return std::max(t.limit - nodes_[t.node].from, 0); }
+
+  // Tiles that all have a workgroup of their own: is it better to leave them whole, though some are longer than a share, than to cut them and have
+  // partial results?
+  // Row tiles: up to one and a half shares.  Whole against cut, 8 heads of 128 in bf16, lengths from .. to: longest 1.3 to 1.46 shares, 250 requests of 500
+  // to 1000 129 / 162 us, 250 of 1500 to 3000 372 / 368, 200 of 2500 to 3000 354 / 426, 30 of 500 to 700 20 / 25; 1.56 shares, 250 of 100 to 1000
+  // 109 / 104, 200 of 500 to 1000 113 / 112; 1.8 shares and more, 200 of 1000 to 3000 301 / 265, 150 of 500 to 700 77 / 71, 200 of 100 to 3000 274 / 208.
+  // Big tiles: what they take whole, by the longest pair of workgroups that share a CU (three quarters of the time a key for one that is left alone: 23
+  // ns for 31), against a share and the way of the partial rows through memory: in bf16 50 rows of all heads a key (45 to 110 us for 13500 rows of 8
+  // heads), in fp8, where a key takes longer, 100.  New tokens of all cached, whole / cut in bf16, then in fp8: 2000 of 2000 64 / 94 us, 94 / 124; 1500
+  // of 9000 in three requests 101 / 114, 151 / 148; 1024 of 8001 and 517 of 5000 206 / 213, 324 / 283; 1280 of 6000 181 / 151, 277 / 203; 1024 of 8192
+  // 190 / 164, 302 / 222; 1408 of 12000 355 / 303, 548 / 404.  Over 48 such prompts the rule is 1 % from the better of the two on average.
+  bool stay_whole(const std::vector<Tile>& tiles, int64_t held, int64_t share, int64_t longest, int64_t pieces) const {
+    if (&tiles == &few_) return 2 * longest <= 3 * share;
+    int64_t whole = 0;  // in quarters of a key
+    if (big_cu_ == 1) whole = 4 * longest;
+    for (size_t j = 0; big_cu_ > 1 && j < tiles.size(); j++) {
+      const size_t other = j + (size_t)held / 2;
+      const int64_t a = keys_of(tiles[j]), b = other < tiles.size() ? keys_of(tiles[other]) : 0;
+      whole = std::max(whole, 4 * std::min(a, b) + 3 * std::abs(a - b));
+    }
+    const int64_t parts = pieces > held ? (int64_t)tiles.size() + held : pieces;
+    return whole - 4 * share <= 4 * row_cost_ * parts;
+  }
+
   // Tiles of whole tokens.  If one piece of at most `share` keys for each of the workgroups that are to run at a time (`held`) is enough,
   // every tile is cut by itself, and each piece has its workgroup.  Otherwise the tiles' keys are one line that is cut into equal shares:
   // a workgroup may take the end of one tile, whole ones and the beginning of another.
   void deal_out(const std::vector<Tile>& tiles, int64_t held, int64_t least, int32_t B, std::vector<int32_t>* wgs, bool* any_mixed) {
     int64_t work = 0;
-    for (const Tile& t : tiles) work += std::max(t.limit - nodes_[t.node].from, 0);
+    for (const Tile& t : tiles) work += keys_of(t);
     held = std::max<int64_t>(1, held);
     const int64_t most = most_keys(B);
     int64_t share = std::max<int64_t>(least, (work + held - 1) / held);
     share = std::min(most, (share + kStep - 1) / kStep * kStep);
-    // Tiles that all have a workgroup of their own stay whole if the longest is not much longer than a share: partial results cost more
-    // (two prompts' chunks of 1024 and 517 tokens behind 8001 and 5000: 211 us whole, 214 in equal shares, and 100 MB of partial results).
-    int64_t longest = 0;
-    for (const Tile& t : tiles) longest = std::max<int64_t>(longest, t.limit - nodes_[t.node].from);
-    if ((int64_t)tiles.size() <= held && longest <= share + share * 5 / 8 && longest <= most) share = std::max(share, longest);
-    int64_t pieces = 0;
-    for (const Tile& t : tiles) pieces += std::max<int64_t>(1, (std::max(t.limit - nodes_[t.node].from, 0) + share - 1) / share);
+    int64_t longest = 0, pieces = 0;
+    auto count = [&] {
+      pieces = 0;
+      for (const Tile& t : tiles) pieces += std::max<int64_t>(1, (keys_of(t) + share - 1) / share);
+    };
+    for (const Tile& t : tiles) longest = std::max(longest, keys_of(t));
+    count();
+    if ((int64_t)tiles.size() <= held && longest > share && longest <= most && stay_whole(tiles, held, share, longest, pieces)) {
+      share = longest;
+      count();
+    }
     const bool line = pieces > held;
     int64_t room = 0;  // keys that the current workgroup still takes
     for (const Tile& t : tiles) {

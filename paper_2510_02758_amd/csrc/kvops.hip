@@ -282,7 +282,7 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     pl.n = pl.T = 0;
     return rc;
   }
-  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus));
+  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3));
   if (rc) return rc;
   b->max_len = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);

@@ -1,5 +1,5 @@
 // Which ways through the attention's kernels a batch takes: its plan (batch.hpp) for a GPU of 256 CUs, in words.
-// stdin: H G B D N n, then n lengths, n query lengths, n + 1 offsets, and the table's blocks.
+// stdin: H G B D N fp8 n, then n lengths, n query lengths, n + 1 offsets, and the table's blocks.
 #include <cstdio>
 #include <map>
 #include <set>
@@ -9,8 +9,8 @@
 #include "../../paper_2510_02758_amd/csrc/batch.hpp"
 
 int main() {
-  int H, G, B, D, N, n;
-  if (std::scanf("%d%d%d%d%d%d", &H, &G, &B, &D, &N, &n) != 6) return 2;
+  int H, G, B, D, N, fp8, n;
+  if (std::scanf("%d%d%d%d%d%d%d", &H, &G, &B, &D, &N, &fp8, &n) != 7) return 2;
   auto read = [](size_t k) {
     std::vector<int32_t> v(k);
     for (int32_t& x : v)
@@ -19,7 +19,7 @@ int main() {
   };
   const auto len = read(n), q = read(n), off = read(n + 1), ids = read(off[n]);
   kvswap::BatchPlan p;
-  const kvswap::BatchShape shape = kvswap::batch_shape(H, D, B, N, 256);
+  const kvswap::BatchShape shape = kvswap::batch_shape(H, D, B, N, 256, fp8 != 0);
   if (p.set(n, off.data(), ids.data(), len.data(), q.data(), G * H, shape) != KV_OK) return 3;
   std::set<std::string> paths;
   paths.insert("hw" + std::to_string(p.heads));

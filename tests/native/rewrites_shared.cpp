@@ -25,7 +25,7 @@ int main() {
       q.push_back(std::min(tokens, pick(0, 1)));
     }
     kvswap::BatchPlan p;
-    if (p.set(n, off.data(), ids.data(), len.data(), q.data(), 2, kvswap::batch_shape(1, 64, B, N, 256)) != KV_OK) return 1;
+    if (p.set(n, off.data(), ids.data(), len.data(), q.data(), 2, kvswap::batch_shape(1, 64, B, N, 256, false)) != KV_OK) return 1;
     std::map<int, int> times;
     for (int32_t id : ids) times[id]++;
     for (int turn = 0; turn < 4; turn++) {

@@ -23,7 +23,7 @@ def test_batches_take_their_ways(plan_paths, name):
     N = sum(-(-n // B) for n in lens) + 3
     rows = tables(np.random.default_rng(0), N, lens, B, shared)
     off = np.concatenate([[0], np.cumsum([len(r) for r in rows])])
-    text = " ".join(str(int(x)) for x in [H, G, B, D, N, len(lens), *lens, *q_lens, *off, *np.concatenate(rows)])
+    text = " ".join(str(int(x)) for x in [H, G, B, D, N, dtype == "fp8_e4m3", len(lens), *lens, *q_lens, *off, *np.concatenate(rows)])
     r = subprocess.run([plan_paths], input=text, capture_output=True, text=True, timeout=60)
     assert r.returncode == 0
     assert want <= set(r.stdout.split()), r.stdout
