@@ -28,7 +28,7 @@ struct AttnItem {
   int32_t part;     // partial row of row0; -1: the rows are finished here
   // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
   int32_t score, score_row, score_from;
-  int32_t fine;  // big tiles: keys that several requests share.  Their weights are as precise as in row tiles, whatever these requests' number
+  int32_t fine;  // keys that several requests share.  In big tiles their weights are as precise as in row tiles, whatever these requests' number
 };
 // One piece of weight accumulation whose products are computed again: keys [k0, k1) that `count` requests have in common, for the
 // rows of these, requests wreqs[first ..].
@@ -55,6 +55,9 @@ struct BatchShape {
   int big_tile = 128;   // rows of a big tile
   int big_cu = 2;       // workgroups of big tiles that share a CU
   int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
+  // A prefix is shared from so many tokens on, by rows of one row tile and by more rows; the latter if all of them together spare `spared` tokens.
+  int few_prefix = 64, big_prefix = 64;
+  int64_t spared = 0;
 };
 
 // Rows of a big tile: what a wavefront's registers hold of their outputs.
@@ -72,6 +75,16 @@ inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cu
   s.big_cu = D <= 128 ? 2 : 1;
   s.big_wgs = cus * s.big_cu;
   s.key_rows = fp8 ? 100 : 50;
+  // Sharing a prefix costs a join of partial results (3 to 5 us), and for more than 16 rows big tiles, which take 25 us (fp8: 30) however little there is
+  // to do; and repeated reads of a short prefix come from the caches.  Decode steps, 8 heads of 128 with 4 query heads each, prefix shared / read by each
+  // request, bf16 us, then fp8.  Up to 16 rows: 2 requests behind 256 tokens 11.5 / 9.7, 11.0 / 8.6, behind 1024 13.2 / 12.4, 13.2 / 12.3; 32 pairs
+  // behind 256 59.3 / 60.7, 36.8 / 37.4, 32 fours behind 512 68 / 73, 47 / 42, behind 1024 63 / 104, 39 / 58.  More rows: 8 requests behind 1024 25 / 16,
+  // 30 / 14, behind 8192 27 / 46, 31 / 32; 32 behind 1024 30 / 23, 34 / 19, behind 2048 31 / 37, 35 / 31, behind 4096 32 / 70, 37 / 46; 128 behind 512
+  // 60 / 47, 46 / 38, behind 1024 62 / 61, 51 / 48, behind 2048 67 / 89, 53 / 72; 8 eights behind 1024 36 / 44, 36 / 33.  So: from 512 tokens, and from
+  // 1024 where what is spared would take 35 us to read at 6.6 TB/s (57000 tokens of these in bf16).
+  s.few_prefix = 512;
+  s.big_prefix = 1024;
+  s.spared = (int64_t)230000000 / (2 * (int64_t)H * D * (fp8 ? 1 : 2));
   s.big_tile = big_tile(D);
   return s;
 }
@@ -206,7 +219,8 @@ class BatchPlan {
     }
     n = n_;
     T = rows;
-    find_nodes(s.B);
+    const int64_t spared = find_nodes(s, true);
+    if (spared > 0 && spared < s.spared) find_nodes(s, false);
     cut(s);
   }
 
@@ -215,7 +229,10 @@ class BatchPlan {
 
   std::vector<Node> nodes_;
 
-  void find_nodes(int32_t B) {
+  // -> tokens that big tiles do not read again.
+  int64_t find_nodes(const BatchShape& s, bool share_big) {
+    const int32_t B = s.B;
+    int64_t spared = 0;
     nodes_.clear();
     struct Work {
       std::vector<int32_t> reqs;
@@ -244,10 +261,13 @@ class BatchPlan {
         else
           most = 0;  // the root has no block yet
         at = std::max(at, most);
-        // A node costs its rows a partial result each; it is worth it from kShared tokens on that it spares.
-        if ((int64_t)(at - w.from) * B * (int64_t)(w.reqs.size() - 1) >= kShared) {
+        const int64_t keys = (int64_t)(at - w.from) * B;
+        int64_t rows = 0;
+        for (int32_t i : w.reqs) rows += (int64_t)q_len[i] * G;
+        if (rows <= kRowTile ? keys >= s.few_prefix : share_big && keys >= s.big_prefix) {
           nodes_.push_back({w.reqs, w.from * B, at * B});
           w.from = at;
+          if (rows > kRowTile) spared += keys * (int64_t)(w.reqs.size() - 1);
         }
       }
       next.clear();
@@ -272,8 +292,8 @@ class BatchPlan {
         k = e;
       }
     }
+    return spared;
   }
-  static constexpr int64_t kShared = 128;
 
   struct Tile {
     int32_t node, list, tokens, row0, rows, limit, clear;

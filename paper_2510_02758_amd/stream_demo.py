@@ -19,7 +19,7 @@ from . import workloads as W
 class Stream:
     """The serving loop's state: tables, lengths, positions and accumulated weights of every request, and the pool they point into."""
 
-    def __init__(self, device, n=3, budget=160, keep=112, seed=0):
+    def __init__(self, device, n=3, budget=608, keep=560, seed=0):
         self.g = g = W.Geometry(L=4, H=2, D=64, B=16, dtype="bf16", N=128)
         self.n, self.G, self.budget, self.keep, self.device = n, 4, budget, keep, device
         self.Hq, self.width = g.H * self.G, 256
@@ -109,7 +109,7 @@ def run(device="cuda", steps=90, preempt_at=30, seed=0):
     s = Stream(torch.device(device, torch.cuda.current_device()), seed=seed)
     gen = torch.Generator(device="cpu").manual_seed(seed + 1)
     rand = lambda t: torch.randn(t, s.width, generator=gen).to(s.device, torch.bfloat16)  # noqa: E731
-    prefix = 4 * s.g.B
+    prefix = 32 * s.g.B
     s.step([0], rand(prefix), [prefix])  # the system prompt, once
     for i in range(1, s.n):
         s.table[i], s.tokens[i], s.position[i] = list(s.table[0]), prefix, prefix

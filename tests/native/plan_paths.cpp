@@ -35,6 +35,7 @@ int main() {
     const bool mixed = it.clear < it.k1;
     paths.insert(big ? "big" : "rows");
     if (mixed) paths.insert(big ? "big_mixed" : "rows_mixed");
+    if (!big && it.fine) paths.insert("rows_shared");
     if (it.part < 0) paths.insert(big ? "big_whole" : "rows_whole");
     if (!big) continue;
     if (it.fine) paths.insert("fine");

@@ -93,6 +93,21 @@ def test_value_scales_far_apart(gpu, D, new, G, B, io_name):
     assert (np.abs(got - ref)[:seen] <= tol[:seen] + 2.0 ** -25).all(), (np.abs(got - ref) / tol)[:seen].max()
 
 
+def _prefix_blocks(g, n):
+    """Blocks of a prefix long enough for n requests with a row of more than 16 each to share it (kvswap.h), and no fewer than few share."""
+    token = 2 * g.H * g.D * (1 if g.dtype == "fp8_e4m3" else 2)
+    return -(-max(1024, -(-230000000 // (token * (n - 1)))) // g.B)
+
+
+def _behind(rng, prefix, own):
+    """Tables that begin with the same `prefix` blocks and go on with own[i] blocks of their own; the number of blocks."""
+    perm, at, rows = rng.permutation(prefix + sum(own)).astype(np.int32), prefix, []
+    for k in own:
+        rows.append(np.concatenate([perm[:prefix], perm[at:at + k]]))
+        at += k
+    return rows
+
+
 @pytest.mark.parametrize("n", [8, 17, 150])  # row tiles, one big tile, several
 @pytest.mark.parametrize("B,D", [(16, 64), (16, 128), (16, 256), (6, 72)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8_e4m3"])
@@ -100,41 +115,44 @@ def test_rows_behind_a_prefix_are_as_precise_whatever_their_number(gpu, dtype, B
     """Two tokens of a shared prefix with values 1 and -1 and scores 0 and -a, all others without weight: the output is tanh(a/2), a difference of
     weights.  These carry 16 bits and more (2^-16 of their sum), and the output is rounded once."""
     import torch
-    shared, lens = 13, [13 * B + 1] * n
-    N = shared + n + 2
-    p = Pool(gpu, W.Geometry(1, 1, D, B, dtype, N), seed=4)
-    perm = p.rng.permutation(N).astype(np.int32)
-    rows = [np.concatenate([perm[:shared], perm[shared + i:shared + i + 1]]) for i in range(n)]
-    values = torch.zeros(2, N, B, 1, D)
+    H = 4
+    shared = _prefix_blocks(W.Geometry(1, H, D, B, dtype, 1), max(n, 17))
+    N, lens = shared + n, [shared * B + 1] * n
+    p = Pool(gpu, W.Geometry(1, H, D, B, dtype, N), seed=4)
+    rows = _behind(p.rng, shared, [1] * n)
+    first = int(rows[0][0])
+    values = torch.zeros(2, N, B, H, D, device=gpu)
     values[0, ..., 0] = -64.0
-    values[0, int(perm[0]), 0, 0, 0], values[0, int(perm[0]), 1, 0, 0] = 0.0, -1.0
-    values[1, int(perm[0]), 0], values[1, int(perm[0]), 1] = 1.0, -1.0
-    p.bits()[0] = values.to(_torch_type(dtype)).view(torch.uint8 if dtype == "fp8_e4m3" else torch.int16).to(gpu)
+    values[0, first, 0, :, 0], values[0, first, 1, :, 0] = 0.0, -1.0
+    values[1, first, 0], values[1, first, 1] = 1.0, -1.0
+    p.bits()[0] = values.to(_torch_type(dtype)).view(torch.uint8 if dtype == "fp8_e4m3" else torch.int16)
     for io_name in ([dtype] if dtype != "fp8_e4m3" else ["bf16", "f16"]):
-        q = torch.zeros(n, 1, D)
+        q = torch.zeros(n, H, D)
         a = torch.linspace(0.3, 1.5, n).to(_torch_type(io_name))
-        q[:, 0, 0] = a.float()
+        q[:, :, 0] = a.float()[:, None]
         q = q.to(gpu, _torch_type(io_name))
         got = _attend(p, rows, lens, [1] * n, q, 1.0)
+        assert p.batch.query()["read_tokens"] == shared * B + n
         want = np.tanh(a.double().numpy() / 2)[:, None, None]
         tol = R.U[io_name] * want * (1 + 2.0 ** -7) + 2.0 ** -16
         assert (np.abs(got - want) <= tol).all(), (io_name, (np.abs(got - want) / tol).max())
 
 
 ODD = {
-    # H, D, B, G, lens, q_lens, requests that share their first blocks
-    "decode": (2, 128, 16, 4, [300, 70], [1, 1], ()),
-    "decode, d 72": (2, 72, 6, 4, [300, 70], [1, 1], ()),
-    "decode, d 256": (1, 256, 16, 4, [300, 70], [1, 1], ()),
-    "decode, cut": (1, 64, 16, 4, [9000, 70], [1, 1], ()),
-    "two new tokens": (2, 128, 16, 4, [300, 70], [2, 2], ()),
-    "two new tokens, d 256": (1, 256, 16, 4, [300, 70], [2, 2], ()),
-    "many heads": (1, 128, 16, 40, [300, 70], [1, 1], ()),
-    "prompt": (2, 128, 16, 4, [300, 70], [180, 40], ()),
-    "prompt, d 72": (2, 72, 6, 4, [300, 70], [180, 40], ()),
-    "prompt, d 256": (1, 256, 16, 4, [300, 70], [180, 40], ()),
-    "prefix": (2, 64, 16, 4, [300 + i for i in range(9)], [1] * 9, tuple((i, 0, 17) for i in range(1, 9))),
-    "prefix, d 96": (1, 96, 5, 4, [300 + i for i in range(9)], [1] * 9, tuple((i, 0, 55) for i in range(1, 9))),
+    # H, D, B, G, lens, q_lens; lens 0: 40 tokens behind a prefix that all share
+    "decode": (2, 128, 16, 4, [300, 70], [1, 1]),
+    "decode, d 72": (2, 72, 6, 4, [300, 70], [1, 1]),
+    "decode, d 256": (1, 256, 16, 4, [300, 70], [1, 1]),
+    "decode, cut": (1, 64, 16, 4, [9000, 70], [1, 1]),
+    "two new tokens": (2, 128, 16, 4, [300, 70], [2, 2]),
+    "two new tokens, d 256": (1, 256, 16, 4, [300, 70], [2, 2]),
+    "many heads": (1, 128, 16, 40, [300, 70], [1, 1]),
+    "prompt": (2, 128, 16, 4, [300, 70], [180, 40]),
+    "prompt, d 72": (2, 72, 6, 4, [300, 70], [180, 40]),
+    "prompt, d 256": (1, 256, 16, 4, [300, 70], [180, 40]),
+    "prefix, few": (2, 64, 16, 4, [0] * 4, [1] * 4),
+    "prefix": (2, 64, 16, 4, [0] * 17, [1] * 17),
+    "prefix, d 96": (2, 96, 5, 2, [0] * 17, [1] * 17),
 }
 
 
@@ -144,10 +162,15 @@ def test_infinities_among_the_values(gpu, dtype, name):
     """An infinity in a value makes that element of the rows that see it infinite, two of unlike sign or a NaN make it a NaN; other elements, and
     rows that do not see the token, are as without."""
     import torch
-    H, D, B, G, lens, q_lens, shared = ODD[name]
-    N = sum(-(-n // B) for n in lens) + 3
+    H, D, B, G, lens, q_lens = ODD[name]
+    rng = np.random.default_rng(7)
+    if lens[0]:
+        N = sum(-(-n // B) for n in lens) + 3
+        rows = _tables(rng, N, lens, B)
+    else:
+        shared, own = _prefix_blocks(W.Geometry(1, H, D, B, dtype, 1), 17), -(-40 // B)
+        rows, lens, N = _behind(rng, shared, [own] * len(lens)), [shared * B + 40] * len(lens), shared + own * len(lens)
     p = Pool(gpu, W.Geometry(1, H, D, B, dtype, N), seed=7)
-    rows = _tables(p.rng, N, lens, B, shared)
     p.fill(rows, lens)
     q = torch.from_numpy(p.rng.standard_normal((sum(q_lens), H * G, D))).to(_torch_type(dtype)).to(gpu)
     clean, tol, _, _, _, _ = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), D ** -0.5, dtype, B)
@@ -162,6 +185,7 @@ def test_infinities_among_the_values(gpu, dtype, name):
     with np.errstate(invalid="ignore"):
         want, _, _, _, _, _ = R.attention(p.values()[0], rows, lens, q_lens, q.double().cpu().numpy(), D ** -0.5, dtype, B)
     got = _attend(p, rows, lens, q_lens, q, D ** -0.5)
+    assert len(lens) == 2 or p.batch.query()["read_tokens"] < 2 * lens[0]
     assert np.isposinf(want).any() and np.isneginf(want).any() and np.isnan(want).any()
     assert np.array_equal(np.isposinf(got), np.isposinf(want))
     assert np.array_equal(np.isneginf(got), np.isneginf(want))
