@@ -442,6 +442,7 @@ int kv_batch_destroy(kv_batch* b);
  * the stream the batch was set on, and a replay is good until the next kv_batch_set.  The batch does not see when a replay runs, and on
  * which stream.  kv_batch_set and kv_batch_destroy therefore wait on the host for the device if calls have been captured since the batch was
  * set.  Until then the caller keeps replays apart from each other and from direct calls with the batch: they use the same workspaces.
+ * The stream of a call has to live until the next call with the batch that is on another stream, or until kv_batch_destroy.
  * Errors: KV_EINVAL (negative sizes, q_lens[i] > num_tokens[i] except 1 row for 0 tokens, a row too short, a head count that does
  * not fit, a capturing stream), KV_ERANGE (block id): the batch stays as it was; KV_ENOMEM, KV_EHIP: it has no requests. */
 int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens,

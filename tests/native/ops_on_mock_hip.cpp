@@ -229,6 +229,31 @@ void room_is_grown_by_set() {
   CHECK(other.attn(other.s[0], true) == KV_OK && other.evict(other.s[0], 140) == KV_OK && calls() == before + 2);
 }
 
+// A kv_batch_set that fails on the device's side leaves a batch without requests, whose calls do nothing; the next one is good.
+void set_that_fails() {
+  for (int n = 1;; n++) {
+    World w;
+    CHECK(w.set(w.s[0], 2, 300, 7) == KV_OK && w.attn(w.s[0], true) == KV_OK && w.evict(w.s[1], 140) == KV_OK);
+    CHECK(hipStreamSynchronize(w.s[0]) == hipSuccess && hipStreamSynchronize(w.s[1]) == hipSuccess);
+    mockhip::fail_after(n, hipErrorInvalidValue);
+    const int rc = w.set(w.s[2], 40, 9000, 7);
+    const bool fired = mockhip::failure_fired();
+    mockhip::fail_after(0, 0);
+    if (!fired) {
+      CHECK(rc == KV_OK && n > 4);
+      return;
+    }
+    CHECK(rc == KV_EHIP && w.pool.last_hip == hipErrorInvalidValue);
+    tables_seen.clear();
+    launched.clear();
+    kv_batch_info info{sizeof(kv_batch_info)};
+    CHECK(kv_batch_query(w.b, &info) == KV_OK && info.rows == 0 && info.cached_tokens == 0);
+    CHECK(w.attn(w.s[0], true) == KV_OK && w.append(w.s[0]) == KV_OK && w.evict(w.s[0], 140) == KV_OK && launched.empty());
+    CHECK(w.set(w.s[0], 2, 300, 9) == KV_OK && w.attn(w.s[0], true) == KV_OK && w.evict(w.s[0], 140) == KV_OK && launched.size() >= 2);
+    CHECK(hipStreamSynchronize(w.s[0]) == hipSuccess && (tables_seen == std::vector<int32_t>{9}));
+  }
+}
+
 // A launch has fewer than 2^32 lanes; an eviction that needs more goes through its layers in parts, each selected and moved.
 void launches_of_a_large_eviction() {
   World w(80, 8, 128, 16, 1 << 20);
@@ -285,6 +310,7 @@ int main(int, char** argv) {
   else if (name == "launches_of_a_large_eviction") launches_of_a_large_eviction();
   else if (name == "room_is_grown_by_set") room_is_grown_by_set();
   else if (name == "far_positions") far_positions();
+  else if (name == "set_that_fails") set_that_fails();
   else return 2;
   std::printf("ok\n");
   return 0;
