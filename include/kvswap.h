@@ -538,7 +538,7 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream);
  * block that stays, whose scales kv_append would replace.
  * weights [num_layers][n][H][weights_cap]; weights_out the same (NULL or the same pointer: in place).
  * req_ids (host, nullable) [n]: requests that the staging arena may hold copies of; their watermark and staged blocks go back to the
- * blocks that have not changed, and they leave the write queue.
+ * blocks that have not changed, and they leave the write queue (at the call: KV_EINVAL in a capture, whose replays would come later).
  * Errors: KV_EINVAL (also 2^23 heads of requests and more); KV_EDUP: a block that would be written (from index keep_first / B on) is in the batch a second time;
  * KV_EEXIST: a request of req_ids is swapped out; KV_EHIP. */
 typedef struct {

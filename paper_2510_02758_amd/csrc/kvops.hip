@@ -570,6 +570,8 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
   if (crowded && pl.rewrites_shared(a->keep, fixed_blocks, keep_blocks)) return KV_EDUP;
   std::vector<int32_t> unchanged;
   if (a->req_ids) {
+    // what becomes of host copies is settled now: a replay would come after copies that have been made since
+    if (!v.plan_only && is_capturing((hipStream_t)stream)) return KV_EINVAL;
     rc = kvswap::pool_may_rewrite(b->pool, pl.n, a->req_ids);
     if (rc) return rc;
     for (int32_t i = 0; i < pl.n; i++) unchanged.push_back(pl.len[i] > a->keep ? fixed_blocks : -1);

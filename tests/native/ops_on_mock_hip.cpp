@@ -68,7 +68,8 @@ int pool_view(kv_pool* p, PoolView* out) { return *out = p->v, KV_OK; }
 int pool_usable(kv_pool*) { return KV_OK; }
 void pool_hip_error(kv_pool* p, int code) { p->last_hip = code; }
 int pool_may_rewrite(kv_pool*, int32_t, const uint64_t*) { return KV_OK; }
-void pool_rewritten(kv_pool*, int32_t, const uint64_t*, const int32_t*) {}
+long rewritten = 0;
+void pool_rewritten(kv_pool*, int32_t, const uint64_t*, const int32_t*) { rewritten++; }
 }  // namespace kvswap
 
 #define CHECK(cond)                                                      \
@@ -128,7 +129,7 @@ struct World {
     a.k = a.v = kSomewhere;
     return kv_append(b, &a, st);
   }
-  int evict(hipStream_t st, int32_t keep) {
+  int evict(hipStream_t st, int32_t keep, const uint64_t* req_ids = nullptr) {
     kv_evict_args a{};
     a.struct_size = sizeof(a);
     a.num_layers = pool.v.L;
@@ -136,6 +137,7 @@ struct World {
     a.weights = (const float*)kSomewhere;
     a.kept = (int32_t*)kSomewhere;
     a.weights_cap = 1 << 30;
+    a.req_ids = req_ids;
     return kv_evict(b, &a, st);
   }
   ~World() {
@@ -254,6 +256,18 @@ void set_that_fails() {
   }
 }
 
+// Host copies go stale when an eviction's call says so, which a replay cannot: none is captured with requests.
+void captured_evictions_have_no_requests() {
+  World w;
+  const uint64_t ids[2] = {5, 6};
+  CHECK(w.set(w.s[0], 2, 300) == KV_OK && w.evict(w.s[0], 140, ids) == KV_OK && kvswap::rewritten == 1);
+  const size_t before = launched.size();
+  mockhip::begin_capture(w.s[0]);
+  CHECK(w.evict(w.s[0], 140, ids) == KV_EINVAL && launched.size() == before && kvswap::rewritten == 1);
+  CHECK(w.evict(w.s[0], 140) == KV_OK && launched.size() == before + 2);
+  mockhip::end_capture();
+}
+
 // A launch has fewer than 2^32 lanes; an eviction that needs more goes through its layers in parts, each selected and moved.
 void launches_of_a_large_eviction() {
   World w(80, 8, 128, 16, 1 << 20);
@@ -311,6 +325,7 @@ int main(int, char** argv) {
   else if (name == "room_is_grown_by_set") room_is_grown_by_set();
   else if (name == "far_positions") far_positions();
   else if (name == "set_that_fails") set_that_fails();
+  else if (name == "captured_evictions_have_no_requests") captured_evictions_have_no_requests();
   else return 2;
   std::printf("ok\n");
   return 0;

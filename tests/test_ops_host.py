@@ -23,7 +23,8 @@ def ops(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["replay_then_set", "captures_draw_no_tickets", "an_earlier_error", "launches_of_a_large_eviction", "room_is_grown_by_set", "far_positions", "set_that_fails"])
+@pytest.mark.parametrize("name", ["replay_then_set", "captures_draw_no_tickets", "an_earlier_error", "launches_of_a_large_eviction", "room_is_grown_by_set", "far_positions", "set_that_fails",
+                                  "captured_evictions_have_no_requests"])
 def test_host_side(ops, name):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:detect_stack_use_after_return=0")
     r = subprocess.run([ops, name], capture_output=True, text=True, timeout=120, env=env)
