@@ -1,0 +1,578 @@
+"""What speculative decoding and multi-axis positions on the paged KV pool are measured on: one call for one layer (acceptance:
+for all layers) of a serving loop whose requests draft trees of tokens, over the batches such a loop meets.
+
+  tree    attention of every request's drafted tokens over its cached tokens and over their own ancestors in the tree
+  accept  the path of drafted tokens that the model agrees with is found, and its keys and values move to the front of the
+          drafted ones, in all layers
+  axes    rotary positions that have several axes (time, height, width) for queries and keys, with keys and values written
+          into the blocks of the batch's requests
+
+With `own` false the operators are computed in their plain form, in 32 bits, from elementary torch operations.  Shapes are
+those of workloads.py and generic ones (odd head sizes and block sizes).
+"""
+import math
+
+import torch
+
+own = False
+
+_DTYPE = {"f16": torch.float16, "bf16": torch.bfloat16, "fp8_e4m3": torch.float8_e4m3fn}
+_VOCABULARY = 32000
+
+
+def _shape(L, H, D, B, dtype, G, scales=False):
+    return dict(L=L, H=H, D=D, B=B, dtype=dtype, G=G, scales=scales)
+
+
+_TINY = _shape(2, 4, 64, 16, "f16", 2)
+_LLAMA8B = _shape(2, 8, 128, 16, "bf16", 4)
+_LLAMA70B = _shape(2, 8, 128, 16, "bf16", 8)
+_FP8_MHA = _shape(2, 32, 128, 32, "fp8_e4m3", 1, scales=True)
+_ONE_HEAD = _shape(2, 1, 128, 16, "bf16", 8)
+
+
+def _batch(n, lo, hi, q_lo, q_hi, prefix=0):
+    """n requests of lo..hi tokens of their own behind `prefix` shared ones, the last q_lo..q_hi of them new."""
+    return dict(n=n, lo=lo, hi=hi, q_lo=q_lo, q_hi=q_hi, prefix=prefix)
+
+
+def _tree(name, shape, batch, levels, unused=0, weights=False):
+    """Trees of that many levels behind their first row; the last `unused` rows of every request are not in its tree."""
+    c = dict(op="tree", **shape, **batch, levels=levels, unused=unused, weights=weights)
+    return dict(c, name=name) if name else c
+
+
+def _accept(name, shape, batch, levels, most):
+    """Of every tree a path of 1 .. most rows is accepted."""
+    c = dict(op="accept", **shape, **batch, levels=levels, unused=0, most=most)
+    return dict(c, name=name) if name else c
+
+
+def _axes(name, shape, batch, rot, interleaved, axes, order):
+    """order: "sections": each axis has a run of neighbouring pairs; "turns": the axes take the pairs in turn."""
+    c = dict(op="axes", **shape, **batch, rot=rot, interleaved=interleaved, axes=axes, order=order)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # Small trees of a toy model, padded to one size: what a call costs.
+        _tree("tiny_tree", _TINY, _batch(8, 16, 256, 1, 9), 3, unused=1),
+        # A burst of ordinary requests that draft eight tokens each: few rows, bound by reading the cache.
+        _tree("llama8b_tree_burst", _LLAMA8B, _batch(64, 512, 4096, 8, 8), 4),
+        # Few requests that draft large trees.
+        _tree("llama8b_large_trees", _LLAMA8B, _batch(4, 1500, 9001, 60, 64), 8),
+        # Trees of requests behind one long system prompt.
+        _tree("llama70b_tree_shared_prefix", _LLAMA70B, _batch(48, 40, 900, 16, 16, prefix=4096), 5),
+        # Trees on an fp8 pool with scales, a query head for every KV head.
+        _tree("fp8_tree", _FP8_MHA, _batch(32, 256, 8192, 17, 32), 6, unused=2),
+        # One very long request on a tensor-parallel shard with one KV head.
+        _tree("one_head_long_tree", _ONE_HEAD, _batch(1, 120001, 120001, 48, 48), 8),
+        # Acceptance on a toy model: what a call costs.
+        _accept("tiny_accept", _TINY, _batch(8, 16, 256, 2, 9), 3, 4),
+        # Acceptance of ordinary requests in all layers.
+        _accept("llama8b_accept", dict(_LLAMA8B, L=32), _batch(64, 90, 400, 24, 32), 7, 8),
+        # Large trees, long paths, an fp8 pool with scales.
+        _accept("fp8_accept", dict(_FP8_MHA, L=16), _batch(24, 200, 500, 48, 64), 16, 16),
+        # One decode step of a toy model with two axes: what a call costs.
+        _axes("tiny_axes", _TINY, _batch(8, 16, 256, 1, 1), 64, True, 2, "turns"),
+        # Prompts with images go into the cache.
+        _axes("llama8b_axes_prompts", _LLAMA8B, _batch(3, 2000, 5001, 1031, 1801), 128, False, 3, "sections"),
+        # Drafted tokens of a large batch behind images, on an fp8 pool with scales.
+        _axes("fp8_axes_drafts", _FP8_MHA, _batch(96, 64, 256, 8, 8), 128, False, 3, "turns"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    shape = rng.choice([_TINY, _LLAMA8B, _LLAMA70B, _FP8_MHA, _ONE_HEAD, None, None, None, None])
+    if shape is None:
+        dtype = rng.choice(["f16", "bf16", "fp8_e4m3"])
+        shape = _shape(2, rng.choice([1, 2, 3, 4, 5, 8, 16]), rng.choice([64, 80, 96, 112, 128, 192, 256]), rng.choice([1, 4, 8, 16, 20, 32]), dtype,
+                       rng.choice([1, 2, 3, 4, 5, 7, 8]), scales=dtype == "fp8_e4m3" and rng.random() < 0.6)
+    row = 2 * shape["H"] * shape["D"] * (1 if shape["dtype"] == "fp8_e4m3" else 2)  # bytes of a token in a layer
+    op = rng.choice(["tree", "tree", "tree", "accept", "axes"])
+    if op == "axes":
+        n = _log(rng, 1, 300)
+        q = _log(rng, 1, max(1, min(4000, 4500 // n)))
+        axes = rng.choice([2, 3, 4])
+        rot = shape["D"] if rng.random() < 0.6 else 2 * rng.randint(axes, shape["D"] // 2)
+        hi = q + _log(rng, 1, 500)
+        return _axes(None, shape, _batch(n, rng.randint(q, hi), hi, rng.randint(1, q), q), rot, rng.random() < 0.5, axes, rng.choice(["sections", "turns"]))
+    if op == "accept":
+        q = _log(rng, 2, 100)
+        n = _log(rng, 1, 64)
+        hi = q + _log(rng, 1, max(2, min(1000, (1 << 25) // (row * n))))
+        shape = dict(shape, L=2 * rng.randint(1, max(1, min(16, (1 << 29) // (row * hi * n)))))
+        levels = rng.randint(1, max(1, min(q - 1, 20)))
+        return _accept(None, shape, _batch(n, rng.randint(q, hi), hi, rng.randint(max(2, q // 2), q), q), levels, rng.randint(1, levels + 1))
+    rows = shape["H"] * shape["G"]
+    q = _log(rng, 2, 80)
+    levels = rng.randint(1, max(1, min(q - 1, 10)))
+    unused = rng.choice([0, 0, 1, q // 4])
+    if rng.random() < 0.3:  # many requests behind one prefix
+        n = _log(rng, 2, 50)
+        own_hi = q + _log(rng, 2, max(3, min(1000, (1 << 28) // (row * n))))
+        prefix = _log(rng, 32, max(33, min(4096, int(4e10 / (4.0 * n * q * rows * shape["D"])))))
+        return _tree(None, shape, _batch(n, rng.randint(q, own_hi), own_hi, max(1, q // 2), q, prefix=max(1, prefix // shape["B"]) * shape["B"]), levels,
+                     unused, rng.random() < 0.15)
+    n = _log(rng, 1, 100)
+    hi = q + _log(rng, 8, max(9, min(100000, (1 << 29) // (row * n), int(4e10 / (4.0 * n * q * rows * shape["D"])))))
+    return _tree(None, shape, _batch(n, rng.randint(q, hi), hi, rng.randint(1, q), q), levels, unused, rng.random() < 0.2)
+
+
+# ------------------------------------------------------------------ sizes of a case (the same for every seed)
+
+def _between(n, lo, hi, step):
+    """n whole numbers spread evenly over lo..hi, both reached, in a mixed order."""
+    if n == 1:
+        return [hi]
+    while math.gcd(step, n) > 1:
+        step += 1
+    return [lo + (hi - lo) * ((i * step) % n) // (n - 1) for i in range(n)]
+
+
+def _lengths(case):
+    """Per request: cached tokens with the shared and the new ones, and the new ones."""
+    lens = _between(case["n"], case["lo"], case["hi"], 7)
+    new = _between(case["n"], case["q_lo"], case["q_hi"], 5)
+    return [case["prefix"] + x for x in lens], [min(q, x) for q, x in zip(new, lens)]
+
+
+def _levels(case, q):
+    """Level of each of q rows, -1 for those that are not in the tree: row 0 alone on level 0, the others spread evenly, each
+    level in front of the next."""
+    used = max(1, q - case["unused"])
+    levels = min(case["levels"], used - 1)
+    return [0] + [1 + (j - 1) * levels // (used - 1) for j in range(1, used)] + [-1] * (q - used)
+
+
+def _accepted(case, new):
+    """Rows of each request's accepted path."""
+    most = _between(case["n"], 1, case["most"], 3)
+    return [min(k, max(_levels(case, q)) + 1) for k, q in zip(most, new)]
+
+
+def _elem(case):
+    return 1 if case["dtype"] == "fp8_e4m3" else 2
+
+
+def work(case):
+    lens, new = _lengths(case)
+    H, D, G, e = case["H"], case["D"], case["G"], _elem(case)
+    T = sum(new)
+    if case["op"] == "axes":  # q in and out, k and v in and out
+        return {"bytes": T * (D * (2 * H * G * 2 + 2 * H * (2 + e)) + 4 * case["axes"]), "flops": 3 * T * (H * G + H) * case["rot"]}
+    if case["op"] == "tree":
+        tokens = case["prefix"] + sum(x - case["prefix"] for x in lens)
+        pairs = sum(sum(x - q + 1 + d for d in _levels(case, q) if d >= 0) for x, q in zip(lens, new))
+        nbytes = tokens * 2 * H * D * e + T * H * G * (2 * 2 * D + 4)
+        if case["scales"]:
+            nbytes += -(-tokens // case["B"]) * 2 * H * 4
+        if case["weights"]:
+            nbytes += sum(lens) * H * 8
+        return {"bytes": nbytes, "flops": 4 * pairs * H * G * D}
+    moved = sum(k - 1 for k in _accepted(case, new))
+    return {"bytes": moved * case["L"] * 2 * 2 * H * D * e + T * 12, "flops": 0}
+
+
+# ------------------------------------------------------------------ rotary frequencies
+
+def _frequencies(rot):
+    """Turns a position for each of the rot / 2 pairs."""
+    return [500000.0 ** (-2.0 * j / rot) / (2 * math.pi) for j in range(rot // 2)]
+
+
+def _fixed(f):
+    """Turns in units of 2^-64, as signed 64-bit words: products with a position wrap around once a turn."""
+    out = []
+    for x in f:
+        w = int(round(math.ldexp(math.fmod(x, 1.0), 64))) & ((1 << 64) - 1)
+        out.append(w - (1 << 64) if w >> 63 else w)
+    return out
+
+
+def _pair_axes(case):
+    pairs, axes = case["rot"] // 2, case["axes"]
+    if case["order"] == "turns":
+        return [j % axes for j in range(pairs)]
+    first = pairs // (axes + 1)  # time has fewer pairs than height and width
+    rest = pairs - first
+    return [0] * first + [1 + j * (axes - 1) // rest for j in range(rest)]
+
+
+# ------------------------------------------------------------------ inputs
+
+class _State:
+    pass
+
+
+def _fill(x, gen, dtype, size):
+    """Normal values of standard deviation `size`."""
+    if dtype == "fp8_e4m3":
+        x.copy_((torch.randn(x.shape, generator=gen, device="cuda", dtype=torch.bfloat16) * size).clamp_(-448, 448))
+    else:
+        x.normal_(0.0, size, generator=gen)
+
+
+def _draft(s, host):
+    """Parents of every row, as the drafts of a step come out of it: a row of a level hangs on some row of the level in front."""
+    c, parents = s.case, []
+    for q in s.new:
+        at = _levels(c, q)
+        below = {}
+        for j, d in enumerate(at):
+            below.setdefault(d, []).append(j)
+        pick = torch.rand(q, generator=host).tolist()
+        for j, d in enumerate(at):
+            parents.append(-1 if d == 0 else -2 if d < 0 else below[d - 1][int(pick[j] * len(below[d - 1]))])
+    s.parents_host = parents
+    s.parents = torch.tensor(parents, dtype=torch.int32, device="cuda")
+    # for the plain form, by request and row: parents (behind a request's rows: none), and what a row has in front of it in its tree
+    s.parent = torch.full((c["n"], s.max_q), -2, device="cuda")
+    s.parent[s.req, s.row] = s.parents.long()
+    s.in_tree = s.parent > -2
+    one = torch.eye(s.max_q, device="cuda")
+    up = (s.parent[..., None] == torch.arange(s.max_q, device="cuda")).float()
+    family = one.expand(c["n"], -1, -1)
+    for _ in range(max(max(_levels(c, q)) for q in s.new)):
+        family = torch.clamp(torch.matmul(up, family.contiguous()) + one, max=1.0)
+    s.family = (family > 0) & s.in_tree[..., None]
+
+
+def prepare(case, seed):
+    s = _State()
+    s.case = c = case
+    L, H, D, B, G = (c[k] for k in ("L", "H", "D", "B", "G"))
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(int(seed))
+    host = torch.Generator()
+    host.manual_seed(int(seed))
+    s.lens, s.new = _lengths(c)
+    T = sum(s.new)
+    shared = c["prefix"] // B
+    rows = [-(-(x - c["prefix"]) // B) for x in s.lens]
+    used = shared + sum(rows)
+    N = used + 1 + used // 8
+    perm = torch.randperm(N, generator=host, dtype=torch.int64).to(torch.int32)
+    ids, off, at = [], [0], shared
+    for r in rows:
+        ids.append(torch.cat([perm[:shared], perm[at:at + r]]))
+        at += r
+        off.append(off[-1] + shared + r)
+    s.ids, s.off = torch.cat(ids).numpy(), torch.tensor(off, dtype=torch.int32).numpy()
+    dtype = _DTYPE[c["dtype"]]
+    s.io = torch.bfloat16 if c["dtype"] != "f16" else torch.float16
+    s.pool = torch.empty(L, 2, N, B, H, D, dtype=dtype, device="cuda")
+    for layer in range(L):
+        _fill(s.pool[layer], gen, c["dtype"], 40.0 if c["dtype"] == "fp8_e4m3" else 1.0)
+    s.scale = torch.empty(L, 2, N, H, device="cuda").uniform_(0.02, 0.03, generator=gen) if c["scales"] else None
+    s.layer = L - 1
+
+    # what the plain form and the library's handle need of the batch, on the GPU: the table row by row, padded
+    width = max(off[i + 1] - off[i] for i in range(c["n"]))
+    table = torch.zeros(c["n"], max(1, width), dtype=torch.int64)
+    for i in range(c["n"]):
+        table[i, :off[i + 1] - off[i]] = torch.from_numpy(s.ids[off[i]:off[i + 1]]).long()
+    s.table = table.cuda()
+    s.len = torch.tensor(s.lens, device="cuda")
+    s.q_len = torch.tensor(s.new, device="cuda")
+    s.max_len, s.max_q = max(s.lens), max(s.new)
+    first = torch.tensor([0] + s.new[:-1]).cumsum(0)
+    s.first_row = first.cuda()
+    req = torch.repeat_interleave(torch.arange(c["n"]), torch.tensor(s.new))
+    s.req = req.cuda()
+    s.row = (torch.arange(T) - first[req]).cuda()  # number among its request's new ones
+    s.index = (s.len - s.q_len)[s.req] + s.row      # place in the cache
+
+    if c["op"] == "axes":
+        # new tokens come out of one projection: queries, keys and values side by side
+        s.qkv = torch.empty(T, (G + 2) * H, D, dtype=s.io, device="cuda").normal_(0.0, 1.0, generator=gen)
+        s.q, s.k, s.v = s.qkv[:, :G * H], s.qkv[:, G * H:(G + 1) * H], s.qkv[:, (G + 1) * H:]
+        s.q_out = torch.empty(T, G * H, D, dtype=s.io, device="cuda")
+        s.turns = torch.tensor(_fixed(_frequencies(c["rot"])), dtype=torch.int64, device="cuda")
+        s.pair_axes = _pair_axes(c)
+        s.pair_axis = torch.tensor(s.pair_axes, device="cuda")
+        # text, then the rows and columns of an image of some width, then text again
+        ahead = torch.randint(0, 20000, (c["n"],), generator=host).cuda()[s.req]
+        wide = torch.randint(7, 64, (c["n"],), generator=host).cuda()[s.req]
+        image = (s.row >= s.q_len[s.req] // 8) & (s.row < s.q_len[s.req] * 7 // 8)
+        start = s.index + ahead
+        of_axis = [start // 16, start // wide, start % wide, start % 5]
+        s.positions = torch.stack([torch.where(image, ahead + of_axis[a], start) for a in range(c["axes"])]).to(torch.int32).contiguous()
+        s.kv_scale = torch.empty(2, H, device="cuda").uniform_(0.01, 0.02, generator=gen) if c["scales"] else None
+    else:
+        _draft(s, host)
+    if c["op"] == "tree":
+        s.q = torch.empty(T, G * H, D, dtype=s.io, device="cuda").normal_(0.0, 2.0, generator=gen)
+        s.out = torch.empty(T, G * H, D, dtype=s.io, device="cuda")
+        s.lse = torch.empty(T, G * H, device="cuda")
+        s.softmax_scale = D ** -0.5
+        s.weights = torch.empty(c["n"], H, s.max_len, device="cuda").uniform_(0.0, 1.0, generator=gen) if c["weights"] else None
+    if c["op"] == "accept":
+        if s.scale is not None:  # a step's tokens are appended with the same scales
+            for i in range(c["n"]):
+                tail = s.table[i, (s.lens[i] - s.new[i]) // B:-(-s.lens[i] // B)]
+                s.scale[:, :, tail] = s.scale[:, :, tail[:1]]
+        # the model's choice follows a path down the tree, then leaves it
+        tokens = torch.randint(0, _VOCABULARY, (T,), generator=host).tolist()
+        chosen = torch.randint(0, _VOCABULARY, (T,), generator=host).tolist()
+        pick = torch.rand(T, generator=host).tolist()
+        t = 0
+        for q, k in zip(s.new, _accepted(c, s.new)):
+            parents, at = s.parents_host[t:t + q], _levels(c, q)
+            path = [j for j in range(q) if at[j] == k - 1]  # any row of that level is the last of a path of k rows
+            u = path[int(pick[t] * len(path))]
+            taken = {tokens[t + j] for j in range(q) if parents[j] == u}
+            while chosen[t + u] in taken:
+                chosen[t + u] = (chosen[t + u] + 1) % _VOCABULARY
+            while parents[u] >= 0:
+                chosen[t + parents[u]] = tokens[t + u]
+                u = parents[u]
+            t += q
+        s.tokens = torch.tensor(tokens, dtype=torch.int32, device="cuda")
+        s.chosen = torch.tensor(chosen, dtype=torch.int32, device="cuda")
+        s.count = torch.empty(c["n"], dtype=torch.int32, device="cuda")
+        s.next = torch.empty(c["n"], dtype=torch.int32, device="cuda")
+        s.path = torch.full((c["n"], s.max_q), -1, dtype=torch.int32, device="cuda")
+    if own:
+        _handle(s, N)
+    return s
+
+
+def _handle(s, N):
+    """The handle on the pool and the batch that a serving loop keeps: the batch is set once a step and used by every layer."""
+    from paper_2510_02758_amd import kvswap as kv
+    from paper_2510_02758_amd import workloads as W
+    c = s.case
+    g = W.Geometry(c["L"], c["H"], c["D"], c["B"], c["dtype"], N, scales=c["scales"])
+    arena = torch.empty(g.S, dtype=torch.uint8, device="cuda")
+    s.kp = kv.KVPool(g, s.pool.view(torch.uint8).reshape(-1), arena, scale=None if s.scale is None else s.scale.view(torch.uint8).reshape(-1),
+                     flags=kv.KV_STAGING_DEVICE)
+    s.batch = kv.KVBatch(s.kp)
+    s.ok = kv.kv_check
+    if c["op"] == "axes":
+        s.ok(s.batch.set(s.off, s.ids, s.lens, s.new, c["G"] * c["H"]))
+    else:
+        s.ok(s.batch.set_trees(s.off, s.ids, s.lens, s.new, c["G"] * c["H"], s.parents))
+
+
+# ------------------------------------------------------------------ one pass
+
+def run(s):
+    c = s.case
+    if c["op"] == "tree":
+        if own:
+            s.ok(s.batch.attn(s.layer, s.q, s.out, s.softmax_scale, lse=s.lse, weights=s.weights))
+        else:
+            _tree_plain(s)
+        out = {"out": s.out, "lse": s.lse}
+        if s.weights is not None:
+            out["weights"] = s.weights
+        return out
+    if c["op"] == "accept":
+        if own:
+            s.ok(s.batch.accept(0, c["L"], s.tokens, s.chosen, s.count, s.path, s.next))
+        else:
+            _accept_plain(s)
+        return {"count": s.count, "path": s.path, "next": s.next, "pool": s.pool}
+    if own:
+        ks, vs = (None, None) if s.kv_scale is None else (s.kv_scale[0], s.kv_scale[1])
+        s.ok(s.batch.append(s.layer, s.q, s.k, s.v, s.q_out, turns=s.turns, interleaved=c["interleaved"], positions=s.positions,
+                            pair_axes=s.pair_axes, k_scale=ks, v_scale=vs))
+    else:
+        _axes_plain(s)
+    out = {"q": s.q_out, "pool": s.pool}
+    if s.scale is not None:
+        out["scale"] = s.scale
+    return out
+
+
+def _rotate(x, cos, sin, rot, interleaved):
+    x = x.float()
+    a, b = (x[..., :rot:2], x[..., 1:rot:2]) if interleaved else (x[..., :rot // 2], x[..., rot // 2:rot])
+    cos, sin = cos[:, None], sin[:, None]
+    a, b = a * cos - b * sin, b * cos + a * sin
+    turned = torch.stack([a, b], -1).flatten(-2) if interleaved else torch.cat([a, b], -1)
+    return torch.cat([turned, x[..., rot:]], -1)
+
+
+def _axes_plain(s):
+    c = s.case
+    phase = s.positions.long()[s.pair_axis].t() * s.turns[None]  # wraps once a turn
+    angle = (phase >> 40).float() * (2 * math.pi / (1 << 24))
+    cos, sin = angle.cos(), angle.sin()
+    s.q_out.copy_(_rotate(s.q, cos, sin, c["rot"], c["interleaved"]))
+    k, v = _rotate(s.k, cos, sin, c["rot"], c["interleaved"]), s.v.float()
+    block, place = s.table[s.req, s.index // c["B"]], s.index % c["B"]
+    if s.kv_scale is not None:
+        k, v = k / s.kv_scale[0][:, None], v / s.kv_scale[1][:, None]
+        s.scale[s.layer, 0, block] = s.kv_scale[0]
+        s.scale[s.layer, 1, block] = s.kv_scale[1]
+    if c["dtype"] == "fp8_e4m3":  # assigned as the bytes that they are
+        k, v = (x.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for x in (k, v))
+    pool = s.pool.view(torch.uint8) if c["dtype"] == "fp8_e4m3" else s.pool
+    pool[s.layer, 0, block, place] = k.to(pool.dtype)
+    pool[s.layer, 1, block, place] = v.to(pool.dtype)
+
+
+def _gathered(s, which):
+    """The batch's keys or values of the layer as (request, head, place, D) in 32 bits, zero behind each request's last."""
+    c = s.case
+    x = torch.arange(s.max_len, device="cuda")
+    block = s.table[:, x // c["B"]]
+    pool = s.pool[s.layer, which]
+    pool = pool.view(torch.uint8) if c["dtype"] == "fp8_e4m3" else pool  # gathered as the bytes that they are
+    rows = pool[block, x % c["B"]].view(s.pool.dtype).float()
+    if s.scale is not None:
+        rows = rows * s.scale[s.layer, which][block][..., None]
+    return torch.where((x[None] < s.len[:, None])[..., None, None], rows, torch.zeros_like(rows)).transpose(1, 2)
+
+
+def _tree_plain(s):
+    c = s.case
+    n, H, G, D = c["n"], c["H"], c["G"], c["D"]
+    j = torch.arange(s.max_q, device="cuda")
+    real = j[None] < s.q_len[:, None]
+    row = torch.where(real, s.first_row[:, None] + j[None], torch.zeros_like(s.first_row)[:, None])
+    q = s.q[row].float().view(n, s.max_q, H, G, D).permute(0, 2, 1, 3, 4).reshape(n, H, s.max_q * G, D)
+    # a row of the tree sees what was cached before the step, and its ancestors and itself
+    x = torch.arange(s.max_len, device="cuda")
+    new = x[None] - (s.len - s.q_len)[:, None]
+    relative = s.family.gather(2, new.clamp(0, s.max_q - 1)[:, None].expand(-1, s.max_q, -1))
+    seen = (new < 0)[:, None] & s.in_tree[..., None] | (new >= 0)[:, None] & (x[None] < s.len[:, None])[:, None] & relative
+    seen = (seen & real[..., None])[:, None, :, None]  # (n, 1, max_q, 1, max_len)
+    z = torch.matmul(q, _gathered(s, 0).transpose(2, 3)).view(n, H, s.max_q, G, s.max_len) * s.softmax_scale
+    z = z.masked_fill(~seen, -math.inf)
+    m = z.amax(-1, keepdim=True)
+    p = torch.exp(z - torch.where(m == -math.inf, torch.zeros_like(m), m))
+    total = p.sum(-1, keepdim=True)
+    p = p / torch.where(total == 0, torch.ones_like(total), total)
+    o = torch.matmul(p.view(n, H, s.max_q * G, s.max_len), _gathered(s, 1)).view(n, H, s.max_q, G, D)
+    lse = (m + torch.log(total))[..., 0]
+    s.out.copy_(o[s.req, :, s.row].reshape(-1, H * G, D))
+    s.lse.copy_(lse[s.req, :, s.row].reshape(-1, H * G))
+    if s.weights is not None:
+        s.weights += p.sum((2, 3))
+
+
+def _accept_plain(s):
+    c = s.case
+    n, L, B = c["n"], c["L"], c["B"]
+    j = torch.arange(s.max_q, device="cuda")
+    token = torch.full((n, s.max_q), -1, device="cuda")
+    choice = torch.full((n, s.max_q), -1, device="cuda")
+    token[s.req, s.row], choice[s.req, s.row] = s.tokens.long(), s.chosen.long()
+    at = torch.zeros(n, 1, dtype=torch.int64, device="cuda")
+    going = s.in_tree[:, :1]
+    path = torch.where(j[None] == 0, torch.where(going, 0, -1), torch.full((n, s.max_q), -1, device="cuda"))
+    count = going.long()
+    for step in range(1, min(s.max_q, c["levels"] + 1)):
+        fits = (s.parent == at) & (token == choice.gather(1, at)) & going
+        child = torch.where(fits, j[None], s.max_q).amin(1, keepdim=True)
+        going = child < s.max_q
+        at = torch.where(going, child, at)
+        path[:, step:step + 1] = torch.where(going, child, path[:, step:step + 1])
+        count = count + going.long()
+    s.path.copy_(path)
+    s.count.copy_(count[:, 0])
+    s.next.copy_(choice.gather(1, at)[:, 0])
+    # the accepted rows move, as bytes
+    base = (s.len - s.q_len)[:, None]
+    moves = (path >= 0) & (path != j[None])
+    src, dst = torch.where(moves, base + path, 0), torch.where(moves, base + j[None], 0)
+    i, k = moves.nonzero(as_tuple=True)
+    src, dst = src[i, k], dst[i, k]
+    pool = s.pool.view(torch.uint8) if c["dtype"] == "fp8_e4m3" else s.pool
+    rows = pool[:, :, s.table[i, src // B], src % B]
+    if s.scale is not None:  # the block's scale stays: a row that comes with another one is rounded again
+        old, now = s.scale[:, :, s.table[i, src // B]], s.scale[:, :, s.table[i, dst // B]]
+        again = (rows.view(torch.float8_e4m3fn).float() * (old / now)[..., None]).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        rows = torch.where((old == now)[..., None], rows, again)
+    pool[:, :, s.table[i, dst // B], dst % B] = rows
+
+
+# ------------------------------------------------------------------ the definitions in 64 bits
+
+def exact(case, seed):
+    if case["op"] == "accept":
+        return None  # rows are moved, nothing is computed
+    s = prepare(case, seed)
+    return _axes_exact(s) if case["op"] == "axes" else _tree_exact(s)
+
+
+def _axes_exact(s):
+    c = s.case
+    rot, B = c["rot"], c["B"]
+    f = torch.tensor(_frequencies(rot), dtype=torch.float64, device="cuda")
+    turns = torch.stack([s.positions[a].double() * f[j] for j, a in enumerate(s.pair_axes)], 1)
+    turn = torch.polar(torch.ones_like(turns), 2 * math.pi * (turns - turns.round()))[:, None]
+
+    def rotated(x):
+        x = x.double()
+        y = x.clone()
+        if c["interleaved"]:
+            z = torch.complex(x[..., 0:rot:2], x[..., 1:rot:2]) * turn
+            y[..., 0:rot:2], y[..., 1:rot:2] = z.real, z.imag
+        else:
+            z = torch.complex(x[..., :rot // 2], x[..., rot // 2:rot]) * turn
+            y[..., :rot // 2], y[..., rot // 2:rot] = z.real, z.imag
+        return y
+
+    pool = s.pool.double()
+    scale = None if s.scale is None else s.scale.double()
+    block, place = s.table[s.req, s.index // B], s.index % B
+    for kv, x in ((0, rotated(s.k)), (1, s.v.double())):
+        if scale is not None:
+            x = x / s.kv_scale[kv].double()[:, None]
+            scale[s.layer, kv, block] = s.kv_scale[kv].double()
+        pool[s.layer, kv, block, place] = x.clamp(-448, 448) if c["dtype"] == "fp8_e4m3" else x
+    out = {"q": rotated(s.q), "pool": pool}
+    if scale is not None:
+        out["scale"] = scale
+    return out
+
+
+def _tree_exact(s):
+    c = s.case
+    H, G, D, B = c["H"], c["G"], c["D"], c["B"]
+    out = torch.zeros(s.q.shape, dtype=torch.float64, device="cuda")
+    lse = torch.full(s.lse.shape, -math.inf, dtype=torch.float64, device="cuda")
+    weights = None if s.weights is None else s.weights.double()
+    t = 0
+    for i, (length, new) in enumerate(zip(s.lens, s.new)):
+        rows = s.q[t:t + new].double().view(new, H, G, D)
+        blocks = s.table[i, :-(-length // B)]
+        hidden = torch.ones(new, length, dtype=torch.bool)
+        for j in range(new):
+            parent = s.parents_host[t + j]
+            if parent == -1:
+                hidden[j, :length - new] = False
+            elif parent >= 0:
+                hidden[j] = hidden[parent]
+            if parent > -2:
+                hidden[j, length - new + j] = False
+        hidden = hidden.cuda()
+        live = ~hidden.all(-1)
+        for h in range(H):
+            kv = s.pool[s.layer][:, blocks, :, h].double() if c["dtype"] != "fp8_e4m3" else \
+                s.pool.view(torch.uint8)[s.layer][:, blocks, :, h].contiguous().view(torch.float8_e4m3fn).double()
+            if s.scale is not None:
+                kv = kv * s.scale[s.layer][:, blocks, h].double()[..., None, None]
+            kv = kv.reshape(2, -1, D)[:, :length]
+            z = torch.tensordot(rows[:, h], kv[0].t().contiguous(), 1) * s.softmax_scale
+            z = z.masked_fill_(hidden[:, None], -math.inf)[live]
+            l = z.logsumexp(-1)
+            p = (z - l[..., None]).exp()
+            out[t:t + new].view(new, H, G, D)[live, h] = torch.tensordot(p, kv[1].contiguous(), 1)
+            lse[t:t + new].view(new, H, G)[live, h] = l
+            if weights is not None:
+                weights[i, h, :length] += p.sum((0, 1))
+        t += new
+    res = {"out": out, "lse": lse}
+    if weights is not None:
+        res["weights"] = weights
+    return res
