@@ -295,6 +295,7 @@ def prepare(case, seed):
         s.q_out = torch.empty(T, G * H, D, dtype=s.io, device="cuda")
         s.turns = torch.tensor(_fixed(_frequencies(c["rot"])), dtype=torch.int64, device="cuda")
         s.pair_axes = _pair_axes(c)
+        s.pair_axes_host = torch.tensor(s.pair_axes, dtype=torch.int32).numpy()
         s.pair_axis = torch.tensor(s.pair_axes, device="cuda")
         # text, then the rows and columns of an image of some width, then text again
         ahead = torch.randint(0, 20000, (c["n"],), generator=host).cuda()[s.req]
@@ -382,7 +383,7 @@ def run(s):
     if own:
         ks, vs = (None, None) if s.kv_scale is None else (s.kv_scale[0], s.kv_scale[1])
         s.ok(s.batch.append(s.layer, s.q, s.k, s.v, s.q_out, turns=s.turns, interleaved=c["interleaved"], positions=s.positions,
-                            pair_axes=s.pair_axes, k_scale=ks, v_scale=vs))
+                            pair_axes=s.pair_axes_host, k_scale=ks, v_scale=vs))
     else:
         _axes_plain(s)
     out = {"q": s.q_out, "pool": s.pool}
