@@ -406,8 +406,8 @@ const char* kv_strerror(int code);
 
 /* ------------------------------------------------------------ operators on the pool's contents
  * What the model's layers do with the pool between two swaps: keys and values go in (kv_append), the batch's new tokens
- * attend to what is cached (kv_attn), and the cached tokens that were given least weight go out (kv_evict), which leaves
- * fewer blocks to swap.  Here the elements of a chunk have a meaning: chunk(l, c, p) is [B][H][D], element d of head h of
+ * attend to what is cached (kv_attn), of drafted ones those that the model accepts stay (kv_accept), and the cached tokens that were given least
+ * weight go out (kv_evict), which leaves fewer blocks to swap.  Here the elements of a chunk have a meaning: chunk(l, c, p) is [B][H][D], element d of head h of
  * token t of the block at byte ((t*H + h)*D + d)*e.  In a pool with scales an fp8 value stands for itself times the fp32
  * scale of its (layer, K|V, block, head); without, for itself.  D is a multiple of 8, above 128 of 16, and at most 256.
  *
@@ -438,7 +438,7 @@ int kv_batch_create(kv_pool* p, kv_batch** out);
 int kv_batch_destroy(kv_batch* b);
 /* Replaces what the batch describes.  num_q_heads is a multiple of H: query head hq reads KV head hq / (num_q_heads / H).
  * The copies are enqueued on `stream`; earlier calls with the batch on other streams are waited for on the device, as is the
- * copy by later calls on other streams.  `stream` must not be capturing; kv_append, kv_attn and kv_evict may be captured on
+ * copy by later calls on other streams.  `stream` must not be capturing; kv_append, kv_attn, kv_accept and kv_evict may be captured on
  * the stream the batch was set on, and a replay is good until the next kv_batch_set.  The batch does not see when a replay runs, and on
  * which stream.  kv_batch_set and kv_batch_destroy therefore wait on the host for the device if calls have been captured since the batch was
  * set.  Until then the caller keeps replays apart from each other and from direct calls with the batch: they use the same workspaces.
@@ -447,6 +447,22 @@ int kv_batch_destroy(kv_batch* b);
  * not fit, a capturing stream), KV_ERANGE (block id): the batch stays as it was; KV_ENOMEM, KV_EHIP: it has no requests. */
 int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens,
                  const int32_t* q_lens, int32_t num_q_heads, void* stream);
+
+/* The same for requests that draft: the new tokens of request i with trees[i] (HOST, [n]; NULL: of every request) are a tree.  parents (device, [T]) has
+ * for new token j of such a request the number 0 .. j-1 of its parent among the request's new tokens, or KV_TREE_ROOT: it follows on what was
+ * cached before.  A row with any other number, KV_TREE_NONE say, is in no tree (a tree padded to a fixed size), nor are its descendants.
+ * Entries of requests without a tree are not looked at.  parents is read on `stream`, at the call's place there.
+ * From then on, until the batch is set again:
+ *   kv_attn    a row of a tree sees its request's tokens before the new ones, its ancestors and itself.  A row of no tree sees nothing, whatever its
+ *              query holds, and is seen by none.
+ *   kv_append  with positions NULL turns a row of a tree by num_tokens[i] - q_lens[i] + its number of ancestors.  Every new token, in a tree or
+ *              not, goes to its place in the cache as ever.
+ *   kv_accept  see there.
+ * Errors: as kv_batch_set; KV_EINVAL also for a tree of more than KV_TREE_MAX tokens, and parents NULL where a tree has some. */
+enum { KV_TREE_ROOT = -1, KV_TREE_NONE = -2 };
+#define KV_TREE_MAX 1024
+int kv_batch_set_trees(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens, const int32_t* q_lens,
+                       int32_t num_q_heads, const int32_t* trees, const int32_t* parents, void* stream);
 
 /* What kv_batch_set made of it. */
 typedef struct {
@@ -499,6 +515,13 @@ typedef struct {
   const float *k_scale, *v_scale; /* [H] */
 } kv_append_args;
 int kv_append(kv_batch* b, const kv_append_args* a, void* stream);
+
+/* The same for positions with several axes (height and width of images, time before them for video): pair j is turned by
+ * positions[pair_axes[j] * positions_stride + t] * turns[j].  axes is 1 .. KV_MOST_AXES; pair_axes (HOST, read during the call) has rot/2 numbers
+ * 0 .. axes-1, in any order: a run of pairs for each axis, or the axes in turn.  Tokens of text have the same position on all axes.
+ * Errors: as kv_append; KV_EINVAL also for positions or pair_axes NULL where pairs are turned. */
+#define KV_MOST_AXES 4
+int kv_append_axes(kv_batch* b, const kv_append_args* a, int32_t axes, const int32_t* pair_axes, int64_t positions_stride, void* stream);
 
 /* out[t][hq] = sum over the cached tokens x that row t sees of softmax(scale * q[t][hq] . K[x])[x] * V[x]; new token j of a request
  * sees its request's tokens up to its own index.  lse[t][hq] (nullable) is the logarithm of the softmax's sum.  A row
@@ -554,6 +577,39 @@ typedef struct {
   const uint64_t* req_ids; /* HOST */
 } kv_evict_args;
 int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream);
+
+/* What the model accepts of the batch's drafted trees (kv_batch_set_trees), and their keys and values to where they belong.  tokens[t] is the drafted token
+ * of row t, chosen[t] the one that the model chose after it (its most likely one, or a sample).  Row 0 of a request is accepted as it is (its
+ * token was chosen in the step before); of an accepted row the child whose token is the chosen one is accepted too, of several the first.
+ *   count[i]  rows accepted: 0 if row 0 is in no tree, or there is no row
+ *   path[i]   their numbers among the request's new tokens, in order, and -1 behind them up to q_lens[i]
+ *   next[i]   the token chosen after the last of them, which follows them; -1 if count is 0
+ * In layers layer .. layer+num_layers-1 K and V of accepted row path[i][k] move to cache index num_tokens[i] - q_lens[i] + k, within the request's
+ * blocks.  Afterwards request i has num_tokens[i] - q_lens[i] + count[i] tokens, and what lies behind these is to be appended to again; the batch
+ * still describes it as before, so set it again.  In a pool with scales blocks keep theirs, and a row that comes with another one is rounded to it (beyond
+ * +-448 as +-448): kv_append leaves all blocks of a step with the same ones.
+ * weights (nullable) [num_layers][n][H][weights_cap], as for kv_evict: those of accepted rows move along, the places of the others become 0.
+ * New tokens that are no tree follow on each other as they are, and all of them stay: count[i] is q_lens[i] (0 without cached tokens), next[i] what was
+ * chosen after the last; path[i] is left as it was.
+ * req_ids as for kv_evict.  tokens and path may be NULL in a batch without trees.  num_layers 0: nothing moves.
+ * Errors: KV_EINVAL (also path_cap below the largest tree); KV_EDUP: a block that new tokens of a tree are in is in the batch a second time; KV_EEXIST: a
+ * request of req_ids is swapped out; KV_EHIP. */
+typedef struct {
+  uint32_t struct_size;
+  int32_t layer, num_layers;
+  const int32_t* tokens; /* [T] */
+  const int32_t* chosen; /* [T] */
+  int32_t* count;        /* [n] */
+  int32_t* path;         /* [n][path_cap] */
+  int32_t* next;         /* [n] */
+  int64_t path_stride;   /* per request */
+  int64_t path_cap;
+  float* weights;
+  int64_t weights_strides[3]; /* per layer, request, head */
+  int64_t weights_cap;
+  const uint64_t* req_ids; /* HOST */
+} kv_accept_args;
+int kv_accept(kv_batch* b, const kv_accept_args* a, void* stream);
 
 /* ------------------------------------------------------------ measurement helpers
  * Ceilings the swap is compared against (the paper prints no bandwidth figure; Section 5.2 only asks that

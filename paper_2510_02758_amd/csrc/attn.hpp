@@ -54,7 +54,12 @@ struct AttnArgs {
   float* scores;         // null: the products of row tiles are not kept
   int64_t scores_head;   // of one KV head
   int32_t hw;  // heads of a workgroup of row tiles (1, 2 or 4): its wavefronts take one each, and 4 / hw share a head's keys
+  const kvswap::TreeSight* sight;  // null: no request's new tokens are a drafted tree
+  const uint32_t* bits;
 };
+
+// What a tile's rows see of its keys: all, those in front of each row's limit, or what a tree's bits say.
+enum Sees { kAll = 0, kUpTo = 1, kTree = 2 };
 
 template <typename E>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -72,6 +77,7 @@ struct JoinArgs {
   float* lse;
   int64_t lse_ts;
   int32_t H, G, D;
+  const int32_t* limit;  // of a batch with drafted trees: 0 is a row that is in none
 };
 
 struct WeightArgs {
@@ -105,3 +111,8 @@ template <typename E>
 void launch_join(const JoinArgs& j, const kvswap::BatchPlan& pl, hipStream_t st);
 template <typename E>
 void launch_weights(bool fp8, const WeightArgs& w, int items, hipStream_t st);
+// The two for batches with drafted trees, whose kernels are built in files of their own (attn_tree_bf16.hip, attn_tree_f16.hip); the others call them.
+template <typename E>
+void launch_tree_attn(bool fp8, const AttnArgs& a, const kvswap::BatchPlan& pl, hipStream_t st);
+template <typename E>
+void launch_tree_weights(bool fp8, const WeightArgs& w, int items, hipStream_t st);

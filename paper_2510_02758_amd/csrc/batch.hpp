@@ -4,6 +4,9 @@
 // of requests has in common behind its parent's, a leaf what a request has for itself.  Attention over a node's keys is one
 // product with the queries of all its requests; what a row got at the nodes on its way down is joined by its softmax
 // statistics.  Only blocks that lie in front of every new token of all their requests go to shared nodes, so no row of one needs a mask.
+//
+// A request's new tokens follow one another, or are a tree of drafted ones (kv_batch_set_trees): then a row sees what was cached before the step, and
+// its own ancestors.  Which these are is known on the device only, which has a bit for each of them there (TreeReq).
 #pragma once
 
 #include <algorithm>
@@ -38,6 +41,16 @@ struct WeightItem {
 // The same from products that were kept: the request's rows are row0 .. row0+rows-1 of their tile.
 struct ScoreItem {
   int32_t req, k0, k1, score, score_row, score_from, row0, rows;
+};
+
+// A tree's request, for the kernel that finds out what its rows see.  A row has `words` words of 32 bits, an even number, for the keys from `origin` on
+// (what lies in front of it every row of the tree sees), the first of its request's rows at `word`.  words 0: the new tokens follow one another.
+struct TreeReq {
+  int32_t first, rows, base, word, words, origin;
+};
+// The same as a row of the attention needs it; word -1: the row sees the keys in front of its limit.
+struct TreeSight {
+  int32_t word, origin;
 };
 
 // Where a new token goes: place `place` of block `block` (-1: nowhere), cache index `index`.
@@ -94,7 +107,14 @@ class BatchPlan {
   int32_t n = 0, T = 0, G = 1;
   int64_t cached = 0, read = 0;
   std::vector<int32_t> off, ids, len, q_len, q_first;        // per request (off, q_first: n + 1)
-  std::vector<int32_t> tok_req, tok_limit;                   // per row of the tensors: request, keys it sees
+  std::vector<int32_t> tok_req, tok_limit, tok_clear;        // per row of the tensors: request, keys it may see, keys it sees all of
+  // Drafted trees: which requests' new tokens are one (empty: none), and what the device needs to know of these.
+  std::vector<uint8_t> tree;
+  std::vector<TreeReq> tree_reqs;     // per request
+  std::vector<TreeSight> tree_sight;  // per row
+  int64_t tree_words = 0;
+  int32_t tree_units = 0;             // of the request that has the most: rows, times words in a tree
+  bool tree_tails_shared = false;     // a block that a tree's new tokens are in is in the batch a second time
   std::vector<TokenPlace> places;                            // per row
   std::vector<int32_t> lists;                                // the nodes' tokens
   std::vector<AttnItem> items;                               // first those of row tiles, workgroup by workgroup, then those of big tiles
@@ -115,14 +135,20 @@ class BatchPlan {
   static constexpr int32_t kRowTile = 16;
   static constexpr int32_t kWeightKeys = 256, kWeightReqs = 16, kScoreKeys = 1024;
 
+  bool is_tree(int32_t i) const { return !tree.empty() && tree[i]; }
+
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
-          const BatchShape& s) {
+          const BatchShape& s, const uint8_t* trees = nullptr) {
     if (n_ < 0 || num_q_heads <= 0 || num_q_heads % s.H) return KV_EINVAL;
     if (n_ && (!offsets || !tokens || !q_lens || offsets[0] < 0)) return KV_EINVAL;
-    int64_t rows = 0, keys = 0, table = 0;
+    int64_t rows = 0, keys = 0, table = 0, words = 0;
     for (int32_t i = 0; i < n_; i++) {
       if (offsets[i + 1] < offsets[i] || tokens[i] < 0 || q_lens[i] < 0) return KV_EINVAL;
       if (q_lens[i] > tokens[i] && !(tokens[i] == 0 && q_lens[i] == 1)) return KV_EINVAL;
+      if (trees && trees[i]) {
+        if (q_lens[i] > KV_TREE_MAX) return KV_EINVAL;
+        words += (int64_t)q_lens[i] * ((q_lens[i] + 126) / 64 * 2);
+      }
       const int64_t need = ((int64_t)tokens[i] + s.B - 1) / s.B;
       if ((int64_t)offsets[i + 1] - offsets[i] < need) return KV_EINVAL;
       rows += q_lens[i];
@@ -130,6 +156,7 @@ class BatchPlan {
       table += need;
     }
     const int32_t g = num_q_heads / s.H;
+    if (words > INT32_MAX) return KV_EINVAL;
     if (rows * g > INT32_MAX / 4 || table > INT32_MAX || (keys + 16 * (int64_t)n_) * kRowTile / 16 > INT32_MAX) return KV_EINVAL;
     if (table && !blocks) return KV_EINVAL;
     for (int32_t i = 0; i < n_; i++) {
@@ -141,7 +168,7 @@ class BatchPlan {
     n = T = 0;
     blocks_ = s.N;
     try {
-      lay_out(n_, offsets, blocks, tokens, q_lens, g, (int32_t)rows, keys, (size_t)table, s);
+      lay_out(n_, offsets, blocks, tokens, q_lens, g, (int32_t)rows, keys, (size_t)table, s, trees);
     } catch (...) {
       n = T = 0;
       throw;
@@ -152,15 +179,24 @@ class BatchPlan {
   // Would rewriting blocks [first_block, keep_blocks) of the requests with more than `keep` tokens reach a block that the batch has twice?
   // These blocks are marked, then all others looked up: 128 requests behind 8192 tokens, 69260 blocks, 31 us on the host.
   bool rewrites_shared(int32_t keep, int32_t first_block, int32_t keep_blocks) {
-    marked_.resize((size_t)blocks_, 0);
-    auto each = [&](auto what) {  // blocks [from, to) of the table that are rewritten
+    return twice([&](auto what) {
       for (int32_t i = 0; i < n; i++)
         if (len[i] > keep) what(off[i] + first_block, off[i] + keep_blocks);
-    };
-    bool twice = false;
+    });
+  }
+
+ private:
+  std::vector<uint8_t> marked_;  // by block, all 0 between calls
+  int64_t blocks_ = 0;
+
+  // Is a block of the runs [from, to) of the table, which `each` goes through in order, in the table a second time?
+  template <typename Each>
+  bool twice(Each each) {
+    marked_.resize((size_t)blocks_, 0);
+    bool again = false;
     each([&](int32_t from, int32_t to) {
       for (int32_t k = from; k < to; k++) {
-        twice |= marked_[ids[k]];
+        again |= marked_[ids[k]];
         marked_[ids[k]] = 1;
       }
     });
@@ -177,12 +213,8 @@ class BatchPlan {
     each([&](int32_t from, int32_t to) {
       for (int32_t k = from; k < to; k++) marked_[ids[k]] = 0;
     });
-    return twice || hit;
+    return again || hit;
   }
-
- private:
-  std::vector<uint8_t> marked_;  // by block, all 0 between calls
-  int64_t blocks_ = 0;
 
   struct Node {
     std::vector<int32_t> reqs;
@@ -190,7 +222,7 @@ class BatchPlan {
   };
 
   void lay_out(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t g, int32_t rows,
-               int64_t keys, size_t table, const BatchShape& s) {
+               int64_t keys, size_t table, const BatchShape& s, const uint8_t* trees) {
     G = g;
     cached = keys;
     len.assign(tokens, tokens + n_);
@@ -205,6 +237,10 @@ class BatchPlan {
     places.reserve(rows);
     tok_req.reserve(rows);
     tok_limit.reserve(rows);
+    tok_clear.clear();
+    tok_clear.reserve(rows);
+    tree.clear();
+    if (trees) tree.assign(trees, trees + n_);
     for (int32_t i = 0; i < n_; i++) {
       const int32_t need = (int32_t)(((int64_t)tokens[i] + s.B - 1) / s.B);
       ids.insert(ids.end(), blocks + offsets[i], blocks + offsets[i] + need);
@@ -213,7 +249,8 @@ class BatchPlan {
       for (int32_t j = 0; j < q_lens[i]; j++) {
         tok_req.push_back(i);
         const int32_t x = tokens[i] ? tokens[i] - q_lens[i] + j : -1;
-        tok_limit.push_back(x + 1);
+        tok_limit.push_back(is_tree(i) ? tokens[i] : x + 1);
+        tok_clear.push_back(is_tree(i) && tokens[i] ? tokens[i] - q_lens[i] : x + 1);
         places.push_back({x < 0 ? -1 : ids[off[i] + x / s.B], x < 0 ? 0 : x % s.B, x, 0});
       }
     }
@@ -222,10 +259,40 @@ class BatchPlan {
     const int64_t spared = find_nodes(s, true);
     if (spared > 0 && spared < s.spared) find_nodes(s, false);
     cut(s);
+    see_trees(s.B);
   }
 
   // Blocks of request i that every one of its rows sees whole.
-  int32_t open_blocks(int32_t i, int32_t B) const { return len[i] ? (len[i] - q_len[i] + 1) / B : 0; }
+  int32_t open_blocks(int32_t i, int32_t B) const { return len[i] ? (len[i] - q_len[i] + !is_tree(i)) / B : 0; }
+
+  // Bits begin where a step of the attention does (64 keys, counted from the beginning of the request's own node).
+  void see_trees(int32_t B) {
+    tree_reqs.clear();
+    tree_sight.clear();
+    tree_words = 0;
+    tree_units = 0;
+    tree_tails_shared = false;
+    if (tree.empty()) return;
+    std::vector<int32_t> from((size_t)n, 0);
+    for (const Node& node : nodes_)
+      if (node.reqs.size() == 1 && node.to == len[node.reqs[0]]) from[node.reqs[0]] = node.from;
+    for (int32_t i = 0; i < n; i++) {
+      TreeReq r{q_first[i], q_len[i], std::max(len[i] - q_len[i], 0), 0, 0, 0};
+      if (tree[i] && len[i] && q_len[i]) {
+        r.origin = from[i] + (r.base - from[i]) / 64 * 64;
+        r.words = (len[i] - r.origin + 63) / 64 * 2;
+        r.word = (int32_t)tree_words;
+        tree_words += (int64_t)r.words * r.rows;
+      }
+      tree_reqs.push_back(r);
+      tree_units = std::max(tree_units, r.rows * std::max(r.words, 1));
+      for (int32_t j = 0; j < r.rows; j++) tree_sight.push_back({r.words ? r.word + j * r.words : -1, r.origin});
+    }
+    tree_tails_shared = twice([&](auto what) {
+      for (int32_t i = 0; i < n; i++)
+        if (tree[i] && q_len[i] > 1) what(off[i] + (len[i] - q_len[i]) / B, off[i] + (int32_t)(((int64_t)len[i] + B - 1) / B));
+    });
+  }
 
   std::vector<Node> nodes_;
 
@@ -342,7 +409,7 @@ class BatchPlan {
         for (int32_t j = row0 / G; j <= (row0 + tile_rows - 1) / G; j++) {
           const int32_t limit = std::min(node.to, tok_limit[lists[list + at + j]]);
           t.limit = std::max(t.limit, limit);
-          t.clear = std::min(t.clear, limit);
+          t.clear = std::min(t.clear, std::min(node.to, tok_clear[lists[list + at + j]]));
         }
         return t;
       };

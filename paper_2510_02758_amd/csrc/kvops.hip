@@ -1,6 +1,6 @@
-// C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction.
-// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append, two for kv_evict (two for each
-// part of its layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
+// C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction, accepted drafts.
+// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append and kv_accept, two for kv_evict (one and two
+// for each part of their layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
 // and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set and kv_batch_destroy, and nothing is
 // allocated there but the first room for kept products and for the order of moves, when they are first needed.
 #include <hip/hip_runtime.h>
@@ -10,6 +10,9 @@
 #include <mutex>
 #include <new>
 #include <stdexcept>
+#include <type_traits>
+#include <utility>
+#include <vector>
 
 #include "pool_view.hpp"
 #include "attn.hpp"
@@ -17,6 +20,7 @@
 #include "attn_sum.hip.inc"
 #include "append.hip.inc"
 #include "evict.hip.inc"
+#include "tree.hip.inc"
 
 using kvswap::AttnItem;
 using kvswap::BatchPlan;
@@ -45,12 +49,18 @@ struct kv_batch {
   const WeightItem *witems = nullptr, *wrest = nullptr;
   const ScoreItem* sitems = nullptr;
   const TokenPlace* places = nullptr;
+  const kvswap::TreeReq* tree_reqs = nullptr;
+  const kvswap::TreeSight* tree_sight = nullptr;
+  int32_t max_tree = 0;  // rows of the largest tree
 
   // Partial results and, for callers that want weights without lse, the lse.
   char* ws = nullptr;
   size_t ws_cap = 0;
   float *part_o = nullptr, *lse = nullptr;
   float2* part_ml = nullptr;
+  // Drafted trees: parents that can be relied on, positions by depth, what the rows see.
+  int32_t *parent = nullptr, *position = nullptr;
+  uint32_t* bits = nullptr;
 
   // Products of row tiles that the weights are computed from, and tickets of an eviction's chunks.  The first call that wants one of them takes it
   // (not in a capture); from then on kv_batch_set sees to it that there is room for its batch.
@@ -268,9 +278,13 @@ catch (...) {
   return caught();
 }
 
-int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens, const int32_t* q_lens,
-                 int32_t num_q_heads, void* stream) try {
-  if (!b) return KV_EINVAL;
+}  // extern "C"
+
+namespace {
+
+// `trees`: null without drafted ones; else of each request, whether its new tokens are one.
+int set_batch(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens, const int32_t* q_lens,
+              int32_t num_q_heads, const uint8_t* trees, const int32_t* parents, void* stream) {
   int rc = kvswap::pool_usable(b->pool);
   if (rc) return rc;
   hipStream_t st = (hipStream_t)stream;
@@ -282,10 +296,12 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     pl.n = pl.T = 0;
     return rc;
   }
-  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3));
+  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3), trees);
   if (rc) return rc;
-  b->max_len = 0;
+  b->max_len = b->max_tree = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);
+  for (int32_t i = 0; i < pl.n; i++)
+    if (pl.is_tree(i)) b->max_tree = std::max(b->max_tree, pl.q_len[i]);
   if (b->v.plan_only) return KV_OK;
   // a failure from here on leaves a batch that describes nothing: the device does not have what the plan says
   struct Undo {
@@ -305,13 +321,14 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
   const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems), VEC(pl.wrest, b->wrest), VEC(pl.sitems, b->sitems), VEC(pl.wreqs, b->wreqs),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
                         VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
-                        VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join)};
+                        VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join), VEC(pl.tree_reqs, b->tree_reqs), VEC(pl.tree_sight, b->tree_sight)};
 #undef VEC
   size_t need = 0;
   for (const Part& p : parts) need += padded(p.bytes);
   const int H = b->v.H;
   const size_t prows = (size_t)pl.partial_rows * H, lse_n = (size_t)pl.T * H * pl.G;
-  const size_t ws_need = padded(prows * b->v.D * 4) + padded(prows * sizeof(float2)) + padded(lse_n * 4);
+  const size_t tree_rows = pl.tree.empty() ? 0 : padded((size_t)pl.T * 4);
+  const size_t ws_need = padded(prows * b->v.D * 4) + padded(prows * sizeof(float2)) + padded(lse_n * 4) + 2 * tree_rows + padded((size_t)pl.tree_words * 4);
   const int k = b->turn;
   if (need > b->mem_cap) {
     rc = drain(b);
@@ -355,17 +372,57 @@ int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* 
     *p.at = b->mem + at;
     at += padded(p.bytes);
   }
-  b->part_o = (float*)b->ws;
-  b->part_ml = (float2*)(b->ws + padded(prows * b->v.D * 4));
-  b->lse = (float*)(b->ws + padded(prows * b->v.D * 4) + padded(prows * sizeof(float2)));
+  char* room = b->ws;
+  auto next = [&](size_t bytes) { return std::exchange(room, room + padded(bytes)); };
+  b->part_o = (float*)next(prows * b->v.D * 4);
+  b->part_ml = (float2*)next(prows * sizeof(float2));
+  b->lse = (float*)next(lse_n * 4);
+  b->parent = (int32_t*)next(tree_rows);
+  b->position = (int32_t*)next(tree_rows);
+  b->bits = (uint32_t*)next((size_t)pl.tree_words * 4);
   if (at) {
     OPCHK(b, hipMemcpyAsync(b->mem, b->up[k], at, hipMemcpyHostToDevice, st));
     OPCHK(b, hipEventRecord(b->up_ev[k], st));
     b->up_busy[k] = true;
     b->turn = 1 - k;
   }
+  if (!pl.tree.empty() && pl.T) {
+    const TreeArgs t{b->tree_reqs, parents, (pl.tree_units + 255) / 256, b->parent, b->position, (int32_t*)b->limit, b->bits};
+    hipLaunchKernelGGL(kv_tree_kernel, dim3((unsigned)(pl.n * t.chunks)), dim3(256), 0, st, t);
+    OPCHK(b, hipGetLastError());
+  }
   undo.pl = nullptr;
   return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_batch_set(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens, const int32_t* q_lens,
+                 int32_t num_q_heads, void* stream) try {
+  if (!b) return KV_EINVAL;
+  return set_batch(b, n, offsets, block_ids, num_tokens, q_lens, num_q_heads, nullptr, nullptr, stream);
+}
+catch (...) {
+  return caught();
+}
+
+int kv_batch_set_trees(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* block_ids, const int32_t* num_tokens, const int32_t* q_lens,
+                       int32_t num_q_heads, const int32_t* trees, const int32_t* parents, void* stream) try {
+  if (!b || n < 0 || (n && !q_lens)) return KV_EINVAL;
+  std::vector<uint8_t> which((size_t)n);
+  bool rows = false;
+  int64_t units = 0;
+  for (int32_t i = 0; i < n; i++) {
+    which[i] = !trees || trees[i];
+    rows = rows || (which[i] && q_lens[i] > 0);
+    // (as many workgroups as the request that needs most; more than a launch may have: refused)
+    units = std::max<int64_t>(units, which[i] ? (int64_t)q_lens[i] * ((q_lens[i] + 126ll) / 64 * 2) : q_lens[i]);
+  }
+  if (rows && !parents) return KV_EINVAL;
+  if ((units + 255) / 256 * n > kMostWgs) return KV_EINVAL;
+  return set_batch(b, n, offsets, block_ids, num_tokens, q_lens, num_q_heads, n ? which.data() : nullptr, parents, stream);
 }
 catch (...) {
   return caught();
@@ -414,17 +471,29 @@ int kv_rope_freqs(int32_t rot, double base, int32_t kind, double factor, double 
   return KV_OK;
 }
 
-int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
-  if (!b || !a || a->struct_size != sizeof(kv_append_args)) return KV_EINVAL;
+}  // extern "C"
+
+namespace {
+
+// axes 0: positions have one, and every pair is turned by it.
+int append(kv_batch* b, const kv_append_args* a, int32_t axes, const int32_t* pair_axes, int64_t positions_stride, void* stream) {
   int rc = kvswap::pool_usable(b->pool);
   if (rc) return rc;
   const PoolView& v = b->v;
   const BatchPlan& pl = b->plan;
   if (a->layer < 0 || a->layer >= v.L || !io_fits(v, a->io_dtype) || a->rot < 0 || a->rot > v.D || a->rot % 2) return KV_EINVAL;
+  uint32_t packed[8] = {};
+  if (axes) {
+    if (axes < 0 || axes > KV_MOST_AXES || (a->rot && !pair_axes)) return KV_EINVAL;
+    for (int32_t j = 0; j < a->rot / 2; j++) {
+      if (pair_axes[j] < 0 || pair_axes[j] >= axes) return KV_EINVAL;
+      packed[j / 16] |= (uint32_t)pair_axes[j] << j % 16 * 2;
+    }
+  }
   const bool scaled = v.has_scale;
   if (scaled != (a->k_scale != nullptr) || scaled != (a->v_scale != nullptr)) return KV_EINVAL;
   if (pl.T == 0 || pl.n == 0) return KV_OK;
-  if (!a->k || !a->v || (a->q != nullptr) != (a->q_out != nullptr) || (a->rot && !a->turns)) return KV_EINVAL;
+  if (!a->k || !a->v || (a->q != nullptr) != (a->q_out != nullptr) || (a->rot && !a->turns) || (axes && a->rot && !a->positions)) return KV_EINVAL;
   if (v.plan_only) return KV_OK;
   hipStream_t st = (hipStream_t)stream;
   rc = order(b, st);
@@ -441,7 +510,9 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
     k.qos[i] = a->q_out_strides[i];
   }
   k.turns = a->turns;
-  k.positions = a->positions;
+  k.positions = a->positions ? a->positions : pl.tree.empty() ? nullptr : b->position;
+  k.axis_stride = positions_stride;
+  std::memcpy(k.axis, packed, sizeof packed);
   k.k_scale = a->k_scale;
   k.v_scale = a->v_scale;
   k.places = b->places;
@@ -466,14 +537,35 @@ int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
     k.chunks = ((k.Hq + v.H) * k.units + v.H * (v.D / 8) + 255) / 256;
   }
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)pl.T * (wide ? k.chunks : 1)), dim3(256), 0, st, k); };
-  if (wide)
-    f16 ? (fp8 ? go(kv_append_wide_kernel<_Float16, true>) : go(kv_append_wide_kernel<_Float16, false>))
-        : (fp8 ? go(kv_append_wide_kernel<__bf16, true>) : go(kv_append_wide_kernel<__bf16, false>));
-  else
-    f16 ? (fp8 ? go(kv_append_kernel<_Float16, true>) : go(kv_append_kernel<_Float16, false>))
-        : (fp8 ? go(kv_append_kernel<__bf16, true>) : go(kv_append_kernel<__bf16, false>));
+  auto any = [&](auto e, auto p, auto x) {
+    using E = decltype(e);
+    if (wide)
+      go(kv_append_wide_kernel<E, decltype(p)::value, decltype(x)::value>);
+    else
+      go(kv_append_kernel<E, decltype(p)::value, decltype(x)::value>);
+  };
+  auto typed = [&](auto p, auto x) { f16 ? any(_Float16(), p, x) : any(__bf16(), p, x); };
+  auto stored = [&](auto x) { fp8 ? typed(std::true_type(), x) : typed(std::false_type(), x); };
+  axes ? stored(std::true_type()) : stored(std::false_type());
   OPCHK(b, hipGetLastError());
   return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_append(kv_batch* b, const kv_append_args* a, void* stream) try {
+  if (!b || !a || a->struct_size != sizeof(kv_append_args)) return KV_EINVAL;
+  return append(b, a, 0, nullptr, 0, stream);
+}
+catch (...) {
+  return caught();
+}
+
+int kv_append_axes(kv_batch* b, const kv_append_args* a, int32_t axes, const int32_t* pair_axes, int64_t positions_stride, void* stream) try {
+  if (!b || !a || a->struct_size != sizeof(kv_append_args) || axes < 1) return KV_EINVAL;
+  return append(b, a, axes, pair_axes, positions_stride, stream);
 }
 catch (...) {
   return caught();
@@ -528,11 +620,15 @@ int kv_attn(kv_batch* b, const kv_attn_args* a, void* stream) try {
     k.scores = (float*)b->scores.at;
     k.scores_head = pl.scores;
   }
-  const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16;
+  const bool fp8 = v.dtype == KV_FP8_E4M3, f16 = a->io_dtype == KV_F16, trees = !pl.tree.empty();
+  if (trees) {
+    k.sight = b->tree_sight;
+    k.bits = b->bits;
+  }
   f16 ? launch_attn<_Float16>(fp8, k, pl, st) : launch_attn<__bf16>(fp8, k, pl, st);
   OPCHK(b, hipGetLastError());
   if (pl.partial_rows) {
-    JoinArgs j{b->join_off, b->join, b->part_o, b->part_ml, k.out, k.o_ts, k.o_hs, k.lse, k.lse_ts, v.H, pl.G, v.D};
+    JoinArgs j{b->join_off, b->join, b->part_o, b->part_ml, k.out, k.o_ts, k.o_hs, k.lse, k.lse_ts, v.H, pl.G, v.D, trees ? b->limit : nullptr};
     f16 ? launch_join<_Float16>(j, pl, st) : launch_join<__bf16>(j, pl, st);
     OPCHK(b, hipGetLastError());
   }
@@ -653,6 +749,88 @@ int kv_evict(kv_batch* b, const kv_evict_args* a, void* stream) try {
       k.kept += layers * k.ks[0];
       k.pool += layers * k.ls;
       if (k.scale) k.scale += layers * k.sls;
+    }
+  }
+  if (a->req_ids) kvswap::pool_rewritten(b->pool, pl.n, a->req_ids, unchanged.data());
+  return KV_OK;
+}
+catch (...) {
+  return caught();
+}
+
+int kv_accept(kv_batch* b, const kv_accept_args* a, void* stream) try {
+  if (!b || !a || a->struct_size != sizeof(kv_accept_args)) return KV_EINVAL;
+  int rc = kvswap::pool_usable(b->pool);
+  if (rc) return rc;
+  const PoolView& v = b->v;
+  const BatchPlan& pl = b->plan;
+  if (a->layer < 0 || a->num_layers < 0 || a->layer > v.L - a->num_layers) return KV_EINVAL;
+  if (pl.n == 0) return KV_OK;
+  if (!a->count || !a->next || (pl.T && !a->chosen)) return KV_EINVAL;
+  if (b->max_tree && (!a->tokens || !a->path || a->path_cap < b->max_tree)) return KV_EINVAL;
+  if (a->weights && a->weights_cap < b->max_len) return KV_EINVAL;
+  if (a->num_layers && !pl.tree.empty() && pl.tree_tails_shared) return KV_EDUP;
+  const int bytes = v.H * v.D * elem(v), vec = bytes % 16 || (v.has_scale && v.D % 16) ? 8 : 16;
+  AcceptArgs k{};
+  k.cols = (bytes / vec + 255) / 256;
+  k.vecs = (bytes / vec + k.cols - 1) / k.cols;
+  if ((int64_t)pl.n * 2 * k.cols > kMostWgs) return KV_EINVAL;
+  std::vector<int32_t> unchanged;
+  if (a->req_ids) {
+    if (!v.plan_only && is_capturing((hipStream_t)stream)) return KV_EINVAL;
+    rc = kvswap::pool_may_rewrite(b->pool, pl.n, a->req_ids);
+    if (rc) return rc;
+    // the first new token stays where it is
+    for (int32_t i = 0; i < pl.n; i++) unchanged.push_back(pl.is_tree(i) && pl.q_len[i] > 1 ? (pl.len[i] - pl.q_len[i] + 1) / v.B : -1);
+  }
+  if (!v.plan_only) {
+    hipStream_t st = (hipStream_t)stream;
+    rc = order(b, st);
+    if (rc) return rc;
+    const bool trees = !pl.tree.empty();
+    k.reqs = trees ? b->tree_reqs : nullptr;
+    k.parent = b->parent;
+    k.tokens = a->tokens;
+    k.chosen = a->chosen;
+    k.q_first = b->q_first;
+    k.len = b->len;
+    k.off = b->off;
+    k.table = b->table;
+    k.count = a->count;
+    k.path = a->path;
+    k.next = a->next;
+    k.path_stride = a->path_stride;
+    k.n = pl.n;
+    k.H = v.H;
+    k.B = v.B;
+    k.pool = v.pool + a->layer * v.ls;
+    k.ls = v.ls;
+    k.vk = v.ks;
+    k.bs = v.bs;
+    k.row = bytes;
+    k.scale = v.scale ? v.scale + a->layer * v.sls : nullptr;
+    k.sls = v.sls;
+    k.svk = v.sks;
+    k.sbs = v.sbs;
+    k.head = v.D * elem(v);
+    k.weights = a->weights;
+    for (int i = 0; i < 3; i++) k.ws[i] = a->weights_strides[i];
+    // as many layers at a time as one launch may have workgroups for; without trees, or without layers, the counts alone
+    const int64_t layer_wgs = (int64_t)pl.n * 2 * k.cols;
+    const int32_t most = (int32_t)std::min<int64_t>(v.L, std::max<int64_t>(1, kMostWgs / layer_wgs)), all = trees ? a->num_layers : 0;
+    for (int32_t done = 0; done == 0 || done < all; done += most) {
+      k.layers = std::min(most, all - done);
+      const unsigned wgs = k.layers ? (unsigned)(k.layers * layer_wgs) : (unsigned)(pl.n * k.cols);
+      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(256), 0, st, k); };
+      if (v.scale)
+        vec == 16 ? go(kv_accept_kernel<u32x4, true>) : go(kv_accept_kernel<u32x2, true>);
+      else
+        vec == 16 ? go(kv_accept_kernel<u32x4, false>) : go(kv_accept_kernel<u32x2, false>);
+      OPCHK(b, hipGetLastError());
+      k.count = nullptr;  // (told by the first)
+      k.pool += most * k.ls;
+      if (k.scale) k.scale += most * k.sls;
+      if (k.weights) k.weights += most * k.ws[0];
     }
   }
   if (a->req_ids) kvswap::pool_rewritten(b->pool, pl.n, a->req_ids, unchanged.data());

@@ -34,6 +34,7 @@ KV_TUNE_HOST_STORES = 13
 KV_TUNE_LINK_IN_WGS, KV_TUNE_LINK_IN_UNROLL = 14, 15
 KV_F16, KV_BF16, KV_FP8_E4M3 = 0, 1, 2
 KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BASE, KV_ROPE_PARTS, KV_ROPE_YARN = 0, 1, 2, 3, 4
+KV_TREE_ROOT, KV_TREE_NONE, KV_TREE_MAX, KV_MOST_AXES = -1, -2, 1024, 4
 
 EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_swap_out", "kv_swap_out_delta", "kv_swap_in", "kv_evict_and_load", "kv_sync",
            "kv_move_blocks", "kv_move_blocks_noalloc", "kv_req_reserve", "kv_req_release", "kv_req_query", "kv_last_stats",
@@ -41,7 +42,8 @@ EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_swap_out", "kv_swap_out_delt
            "kv_io_stats_get", "kv_budget_blocks", "kv_req_poll", "kv_req_wait", "kv_last_timeline",
            "kv_swap_out_delta_timed", "kv_bench_copy", "kv_bench_copy_scrambled", "kv_bench_link", "kv_bench_link_bidir",
            "kv_wq_post", "kv_wq_drain", "kv_wq_remove", "kv_wq_pending",
-           "kv_batch_create", "kv_batch_destroy", "kv_batch_set", "kv_batch_query", "kv_rope_freqs", "kv_append", "kv_attn", "kv_evict"]
+           "kv_batch_create", "kv_batch_destroy", "kv_batch_set", "kv_batch_query", "kv_rope_freqs", "kv_append", "kv_attn", "kv_evict",
+           "kv_batch_set_trees", "kv_append_axes", "kv_accept"]
 
 
 class kv_pool_config(C.Structure):
@@ -108,6 +110,13 @@ class kv_evict_args(C.Structure):
                 ("req_ids", C.c_void_p)]
 
 
+class kv_accept_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("layer", C.c_int32), ("num_layers", C.c_int32), ("tokens", C.c_void_p),
+                ("chosen", C.c_void_p), ("count", C.c_void_p), ("path", C.c_void_p), ("next", C.c_void_p), ("path_stride", C.c_int64),
+                ("path_cap", C.c_int64), ("weights", C.c_void_p), ("weights_strides", C.c_int64 * 3), ("weights_cap", C.c_int64),
+                ("req_ids", C.c_void_p)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError("libkvswap.so is not built: run `python -c 'import __graft_entry__ as g; g.build()'` "
                       "(hipcc --offload-arch=gfx950) first; there is no fallback path")
@@ -155,6 +164,9 @@ _sig = {
     "kv_append": (C.c_int, [_vp, _vp, _vp]),
     "kv_attn": (C.c_int, [_vp, _vp, _vp]),
     "kv_evict": (C.c_int, [_vp, _vp, _vp]),
+    "kv_batch_set_trees": (C.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp]),
+    "kv_append_axes": (C.c_int, [_vp, _vp, _i32, _vp, _i64, _vp]),
+    "kv_accept": (C.c_int, [_vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -571,6 +583,15 @@ def kv_batch_set(b, offsets, block_ids, num_tokens, q_lens, num_q_heads, stream=
     return _lib.kv_batch_set(b, len(t), _p(o), _p(ids), _p(t), _p(q), int(num_q_heads), stream)
 
 
+def kv_batch_set_trees(b, offsets, block_ids, num_tokens, q_lens, num_q_heads, parents_ptr, trees=None, stream=None):
+    """parents_ptr: device address; trees: host, truth values [n]"""
+    o, ids, t, q = _i32a(offsets), _i32a(block_ids), _i32a(num_tokens), _i32a(q_lens)
+    w = None if trees is None else np.ascontiguousarray(np.asarray(trees, dtype=bool), dtype=np.int32)
+    if not _rows_ok(len(t), o, ids, q) or (w is not None and w.shape != t.shape):
+        return KV_EINVAL
+    return _lib.kv_batch_set_trees(b, len(t), _p(o), _p(ids), _p(t), _p(q), int(num_q_heads), None if w is None else w.ctypes.data, parents_ptr, stream)
+
+
 def kv_batch_query(b):
     """-> (rc, dict)"""
     st = kv_batch_info()
@@ -605,6 +626,19 @@ def kv_evict(b, args, stream=None):
     return _lib.kv_evict(b, C.addressof(args), stream)
 
 
+def kv_append_axes(b, args, axes, pair_axes, positions_stride, stream=None):
+    """args: kv_append_args; pair_axes: host, an axis for each of the rot/2 pairs"""
+    args.struct_size = C.sizeof(kv_append_args)
+    p = _i32a(pair_axes)
+    return _lib.kv_append_axes(b, C.addressof(args), int(axes), p.ctypes.data, int(positions_stride), stream) if 2 * len(p) >= args.rot else KV_EINVAL
+
+
+def kv_accept(b, args, stream=None):
+    """args: kv_accept_args"""
+    args.struct_size = C.sizeof(kv_accept_args)
+    return _lib.kv_accept(b, C.addressof(args), stream)
+
+
 def kv_check(rc, what="kvswap"):
     """Raises KVSwapError unless rc is KV_OK."""
     if rc != KV_OK:
@@ -615,11 +649,13 @@ _IO = {torch.float16: KV_F16, torch.bfloat16: KV_BF16}
 # The argument structures as one packing each, and checks that ask a tensor for as little as possible: the host's share of an append
 # with all its tensors, launch excluded, 5.3 us so, 10.3 with the fields set one by one.
 _APPEND, _ATTN, _EVICT = struct.Struct("@IiiiifPPPPqqqqqqqqPPPP"), struct.Struct("@IiifPPqqqqPqPqqq"), struct.Struct("@IiiiiiPPqqqqPqqqP")
-assert [s.size for s in (_APPEND, _ATTN, _EVICT)] == [C.sizeof(s) for s in (kv_append_args, kv_attn_args, kv_evict_args)]
+_ACCEPT = struct.Struct("@IiiPPPPPqqPqqqqP")
+_ALL_ARGS = (_APPEND, _ATTN, _EVICT, _ACCEPT)
+assert [s.size for s in _ALL_ARGS] == [C.sizeof(s) for s in (kv_append_args, kv_attn_args, kv_evict_args, kv_accept_args)]
 
 
 class KVBatch:
-    """The requests of one step on a KVPool, and the operators on them: append, attn, evict.
+    """The requests of one step on a KVPool, and the operators on them: append, attn, accept, evict.
 
     Tensors are torch tensors on the pool's GPU.  q, q_out, out are [T, num_q_heads, D] and k, v [T, H, D], of any strides with
     a contiguous last dimension; T counts the new tokens of all requests in order.  Calls are enqueued on `stream`
@@ -633,16 +669,16 @@ class KVBatch:
         data = pool._keep[0]
         self.device = data.device if data is not None else None
         self._dev = data.get_device() if data is not None else -1
-        self._describe(0, 0, 0, 0)
-        self._args = C.create_string_buffer(max(s.size for s in (_APPEND, _ATTN, _EVICT)))
+        self._describe(0, 0, 0, 0, 0)
+        self._args = C.create_string_buffer(max(s.size for s in _ALL_ARGS))
         self._at = C.addressof(self._args)
         rc, self.h = kv_batch_create(pool.h)
         if rc:
             self.h = None
             raise KVSwapError(rc, "kv_batch_create")
 
-    def _describe(self, n, T, Hq, max_len):
-        self.n, self.T, self.Hq, self.max_len = n, T, Hq, max_len
+    def _describe(self, n, T, Hq, max_len, max_tree):
+        self.n, self.T, self.Hq, self.max_len, self.max_tree = n, T, Hq, max_len, max_tree
         self._q_shape, self._kv_shape = (T, Hq, self.geom.D), (T, self.geom.H, self.geom.D)
 
     def close(self):
@@ -680,9 +716,25 @@ class KVBatch:
         t, q = _i32a(num_tokens), _i32a(q_lens)
         rc = kv_batch_set(self.h, offsets, block_ids, t, q, num_q_heads, self._stream(stream))
         if rc in (KV_ENOMEM, KV_EHIP):
-            self._describe(0, 0, 0, 0)
+            self._describe(0, 0, 0, 0, 0)
         if rc == KV_OK:
-            self._describe(len(t), int(q.sum()), int(num_q_heads), int(t.max()) if len(t) else 0)
+            self._describe(len(t), int(q.sum()), int(num_q_heads), int(t.max()) if len(t) else 0, 0)
+        return rc
+
+    def set_trees(self, offsets, block_ids, num_tokens, q_lens, num_q_heads, parents, trees=None, stream=None):
+        """The same for requests that draft: parents is int32 [T] on the device; trees says of each request whether its new tokens are a tree (None:
+        those of every request)."""
+        if not self.h or not self.pool.h:
+            return KV_EINVAL
+        t, q = _i32a(num_tokens), _i32a(q_lens)
+        if q.ndim != 1 or not self._fits(parents, torch.int32, (int(q.sum()),)):
+            return KV_EINVAL
+        rc = kv_batch_set_trees(self.h, offsets, block_ids, t, q, num_q_heads, parents.data_ptr(), trees, self._stream(stream))
+        if rc in (KV_ENOMEM, KV_EHIP):
+            self._describe(0, 0, 0, 0, 0)
+        if rc == KV_OK:
+            drafts = q if trees is None else q[np.asarray(trees, dtype=bool)]
+            self._describe(len(t), int(q.sum()), int(num_q_heads), int(t.max()) if len(t) else 0, int(drafts.max()) if len(drafts) else 0)
         return rc
 
     def query(self):
@@ -691,8 +743,10 @@ class KVBatch:
             raise KVSwapError(rc, "kv_batch_query")
         return st
 
-    def append(self, layer, q, k, v, q_out=None, turns=None, interleaved=False, magnitude=1.0, positions=None, k_scale=None, v_scale=None, stream=None):
-        """q may be None; q_out defaults to q itself.  turns: int64 [rot/2] on the device (None: nothing is turned), positions: int32 [T]."""
+    def append(self, layer, q, k, v, q_out=None, turns=None, interleaved=False, magnitude=1.0, positions=None, k_scale=None, v_scale=None,
+               pair_axes=None, stream=None):
+        """q may be None; q_out defaults to q itself.  turns: int64 [rot/2] on the device (None: nothing is turned), positions: int32 [T]; with
+        pair_axes (host, int32 [rot/2]: the axis that each pair is turned by) positions is int32 [axes, T]."""
         dtype, dev, shape, ks, vs = k.dtype, self._dev, self._kv_shape, k.stride(), v.stride()
         io = _IO.get(dtype)
         if not (self.h and self.pool.h and io is not None and k.shape == shape and v.shape == shape and v.dtype is dtype and
@@ -710,7 +764,13 @@ class KVBatch:
             rot, tp = 2 * turns.numel(), turns.data_ptr()
             if turns.dtype is not torch.int64 or turns.get_device() != dev or not turns.is_contiguous():
                 return KV_EINVAL
-        if positions is not None:
+        if pair_axes is not None:
+            if positions is None or positions.dim() != 2 or not self._fits(positions, torch.int32, (positions.shape[0], self.T)):
+                return KV_EINVAL
+            pair_axes, pp = _i32a(pair_axes), positions.data_ptr()
+            if pair_axes.shape != (rot // 2,):
+                return KV_EINVAL
+        elif positions is not None:
             pp = positions.data_ptr()
             if positions.dtype is not torch.int32 or positions.shape != (self.T,) or positions.get_device() != dev or not positions.is_contiguous():
                 return KV_EINVAL
@@ -724,6 +784,8 @@ class KVBatch:
                 return KV_EINVAL
         _APPEND.pack_into(self._args, 0, _APPEND.size, layer, io, rot, 1 if interleaved else 0, magnitude, qp, k.data_ptr(), v.data_ptr(), op,
                           qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qo[0], qo[1], tp, pp, kp, vp)
+        if pair_axes is not None:
+            return _lib.kv_append_axes(self.h, self._at, positions.shape[0], pair_axes.ctypes.data, positions.stride(0), self._stream(stream))
         return _lib.kv_append(self.h, self._at, self._stream(stream))
 
     def attn(self, layer, q, out, scale, lse=None, weights=None, stream=None):
@@ -767,3 +829,32 @@ class KVBatch:
         _EVICT.pack_into(self._args, 0, _EVICT.size, layer, num_layers, keep, keep_first, keep_last, weights.data_ptr(), out,
                          ws[0], ws[1], ws[2], weights.shape[3], kept.data_ptr(), ks[0], ks[1], ks[2], ids)
         return _lib.kv_evict(self.h, self._at, self._stream(stream))
+
+    def accept(self, layer, num_layers, tokens, chosen, count, path, next_token, weights=None, req_ids=None, stream=None):
+        """tokens, chosen: int32 [T]; count, next_token: int32 [n]; path: int32 [n, largest tree or more] (tokens and path may be None in a batch
+        without trees); weights: float32 [num_layers, n, H, cap]; req_ids: host uint64 [n]."""
+        if not self.h or not self.pool.h:
+            return KV_EINVAL
+        tp, pp, ps, cap, wp, ws, wcap, ids = 0, 0, 0, 0, 0, (0, 0, 0), 0, 0
+        if not (self._fits(chosen, torch.int32, (self.T,)) and self._fits(count, torch.int32, (self.n,)) and self._fits(next_token, torch.int32, (self.n,))):
+            return KV_EINVAL
+        if tokens is not None:
+            tp = tokens.data_ptr()
+            if not self._fits(tokens, torch.int32, (self.T,)):
+                return KV_EINVAL
+        if path is not None:
+            if path.dim() != 2 or not self._fits(path, torch.int32, (self.n, path.shape[1])):
+                return KV_EINVAL
+            pp, ps, cap = path.data_ptr(), path.stride(0), path.shape[1]
+        if weights is not None:
+            if weights.dim() != 4 or not self._fits(weights, torch.float32, (num_layers, self.n, self.geom.H, weights.shape[3])):
+                return KV_EINVAL
+            wp, ws, wcap = weights.data_ptr(), weights.stride(), weights.shape[3]
+        if req_ids is not None:
+            req_ids = _u64a(req_ids)
+            if len(req_ids) != self.n:
+                return KV_EINVAL
+            ids = req_ids.ctypes.data
+        _ACCEPT.pack_into(self._args, 0, _ACCEPT.size, layer, num_layers, tp, chosen.data_ptr(), count.data_ptr(), pp, next_token.data_ptr(), ps, cap,
+                          wp, ws[0], ws[1], ws[2], wcap, ids)
+        return _lib.kv_accept(self.h, self._at, self._stream(stream))
