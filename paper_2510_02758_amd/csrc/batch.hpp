@@ -20,7 +20,7 @@
 namespace kvswap {
 
 // One piece of attention work for one KV head: a tile of rows against a run of keys.  Nodes of few rows are tiles of their own (at
-// most kRowTile rows), nodes of more rows are cut into big tiles; either kind is dealt out to workgroups in even shares of keys.
+// most row_tile rows), nodes of more rows are cut into big tiles; either kind is dealt out to workgroups in even shares of keys.
 // Row r of a node is new token tokens[first + r / G] with query head r % G of the group.
 struct AttnItem {
   int32_t table;    // where the row of the table begins that names the blocks of the keys
@@ -67,6 +67,7 @@ struct BatchShape {
   int big_least = 512;
   int big_tile = 128;   // rows of a big tile
   int big_cu = 2;       // workgroups of big tiles that share a CU
+  int row_tile = 16;    // rows of a row tile at most
   int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
   // A prefix is shared from so many tokens on, by rows of one row tile and by more rows; the latter if all of them together spare `spared` tokens.
   int few_prefix = 64, big_prefix = 64;
@@ -76,11 +77,15 @@ struct BatchShape {
 // Rows of a big tile: what a wavefront's registers hold of their outputs.
 constexpr int big_tile(int D) { return D <= 128 ? 128 : 64; }
 
+// Pools that the kernels for whole rows and blocks of 16s serve.
+constexpr bool whole_rows(int D, int B) { return (D == 64 || D == 128 || D == 256) && B % 16 == 0; }
+
 // What a pool's batches are laid out for on a GPU of `cus` compute units.  Two workgroups of row tiles a CU: with three, more places of the pool are
 // read at a time, and each more slowly (64 requests of 512 to 4096 tokens on 8 heads of 128 in bf16: 103 us with two, 122 with three, 140 with
 // one; 32 of 256 to 8192 on 32 heads in fp8: 181, 185, 242).
-inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus, bool fp8) {
+inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus, bool fp8, bool trees = false) {
   BatchShape s;
+  if (trees && whole_rows(D, B)) s.row_tile = 32;
   s.H = H;
   s.B = B;
   s.N = N;
@@ -132,7 +137,7 @@ class BatchPlan {
 
   // Entries of the table that an item may need: its part of the table is held on chip.
   static constexpr int32_t kMaxEntries = 2048;
-  static constexpr int32_t kRowTile = 16;
+  static constexpr int32_t kRowTile = 16;  // rows of a row tile, but for batches with drafts (BatchShape::row_tile)
   static constexpr int32_t kWeightKeys = 256, kWeightReqs = 16, kScoreKeys = 1024;
 
   bool is_tree(int32_t i) const { return !tree.empty() && tree[i]; }
@@ -157,7 +162,7 @@ class BatchPlan {
     }
     const int32_t g = num_q_heads / s.H;
     if (words > INT32_MAX) return KV_EINVAL;
-    if (rows * g > INT32_MAX / 4 || table > INT32_MAX || (keys + 16 * (int64_t)n_) * kRowTile / 16 > INT32_MAX) return KV_EINVAL;
+    if (rows * g > INT32_MAX / 4 || table > INT32_MAX || (keys + 16 * (int64_t)n_) * s.row_tile / 16 > INT32_MAX) return KV_EINVAL;
     if (table && !blocks) return KV_EINVAL;
     for (int32_t i = 0; i < n_; i++) {
       const int64_t need = ((int64_t)tokens[i] + s.B - 1) / s.B;
@@ -331,10 +336,10 @@ class BatchPlan {
         const int64_t keys = (int64_t)(at - w.from) * B;
         int64_t rows = 0;
         for (int32_t i : w.reqs) rows += (int64_t)q_len[i] * G;
-        if (rows <= kRowTile ? keys >= s.few_prefix : share_big && keys >= s.big_prefix) {
+        if (rows <= s.row_tile ? keys >= s.few_prefix : share_big && keys >= s.big_prefix) {
           nodes_.push_back({w.reqs, w.from * B, at * B});
           w.from = at;
-          if (rows > kRowTile) spared += keys * (int64_t)(w.reqs.size() - 1);
+          if (rows > s.row_tile) spared += keys * (int64_t)(w.reqs.size() - 1);
         }
       }
       next.clear();
@@ -413,7 +418,7 @@ class BatchPlan {
         }
         return t;
       };
-      if (rows <= kRowTile) {
+      if (rows <= s.row_tile) {
         Tile t = tile(0, tokens, 0, (int32_t)rows);
         t.score_row = (std::max(t.limit - node.from, 0) + 15) / 16 * 16;
         t.score = (int32_t)(scores / 16);
@@ -439,7 +444,7 @@ class BatchPlan {
       for (int32_t k = node.from; k < node.to; k += kWeightKeys)
         for (int32_t r = 0; r < reqs; r += kWeightReqs) {
           witems.push_back({off[node.reqs[0]], k, std::min(node.to, k + kWeightKeys), first + r, std::min(kWeightReqs, reqs - r), {}});
-          if (rows > kRowTile) wrest.push_back(witems.back());
+          if (rows > s.row_tile) wrest.push_back(witems.back());
         }
       for (size_t j = list; j < lists.size(); j++)
         if (node.to > node.from) seen_[lists[j]]++;

@@ -296,7 +296,7 @@ int set_batch(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* blo
     pl.n = pl.T = 0;
     return rc;
   }
-  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3), trees);
+  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3, trees != nullptr), trees);
   if (rc) return rc;
   b->max_len = b->max_tree = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);
