@@ -67,7 +67,9 @@ struct BatchShape {
   int big_least = 512;
   int big_tile = 128;   // rows of a big tile
   int big_cu = 2;       // workgroups of big tiles that share a CU
-  int row_tile = 16;    // rows of a row tile at most
+  // Batches with drafts: rows of a row tile at most; keys that a workgroup takes at a time, by what it is cut to (0: kStep).
+  int row_tile = 16;
+  int row_step = 0, big_step = 0;
   int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
   // A prefix is shared from so many tokens on, by rows of one row tile and by more rows; the latter if all of them together spare `spared` tokens.
   int few_prefix = 64, big_prefix = 64;
@@ -85,7 +87,11 @@ constexpr bool whole_rows(int D, int B) { return (D == 64 || D == 128 || D == 25
 // one; 32 of 256 to 8192 on 32 heads in fp8: 181, 185, 242).
 inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus, bool fp8, bool trees = false) {
   BatchShape s;
-  if (trees && whole_rows(D, B)) s.row_tile = 32;
+  if (trees && whole_rows(D, B)) {
+    s.row_tile = 32;
+    s.row_step = 32;
+    s.big_step = 64;
+  }
   s.H = H;
   s.B = B;
   s.N = N;
@@ -370,12 +376,14 @@ class BatchPlan {
   struct Tile {
     int32_t node, list, tokens, row0, rows, limit, clear;
     int32_t score = 0, score_row = 0;
+    int32_t fine = 0;
   };
   struct Use {
     int32_t list, tokens, part;  // every row of these tokens has a partial row from here on
   };
   std::vector<Tile> few_, big_, huge_;
   int big_cu_ = 1;
+  int32_t row_tile_ = kRowTile;
   double row_cost_ = 0;  // keys that the partial rows of a big tile's piece cost
   std::vector<int32_t> seen_;  // nodes with keys, per token
   std::vector<Use> uses_;
@@ -400,6 +408,7 @@ class BatchPlan {
     // big tile, its tiles are cut alike instead.
     const int32_t big_tokens = s.big_tile / G;
     big_cu_ = s.big_cu;
+    row_tile_ = s.row_tile;
     row_cost_ = (double)s.big_tile * s.H / s.key_rows;
     for (size_t d = 0; d < nodes_.size(); d++) {
       const Node& node = nodes_[d];
@@ -409,8 +418,10 @@ class BatchPlan {
       read += node.to - node.from;
       const int32_t tokens = (int32_t)lists.size() - list;
       const int64_t rows = (int64_t)tokens * G;
+      const bool node_fine = fine(node);
       auto tile = [&](int32_t at, int32_t n, int32_t row0, int32_t tile_rows) {
         Tile t{(int32_t)d, list + at, n, row0, tile_rows, 0, INT32_MAX};
+        t.fine = node_fine;
         for (int32_t j = row0 / G; j <= (row0 + tile_rows - 1) / G; j++) {
           const int32_t limit = std::min(node.to, tok_limit[lists[list + at + j]]);
           t.limit = std::max(t.limit, limit);
@@ -457,9 +468,11 @@ class BatchPlan {
     // heads of 128 in bf16: 103 us instead of 135, 32 requests of 256 to 8192 with 32 heads in fp8: 175 to 181 instead of 207.
     heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
     wg_items.clear();
+    step_ = s.row_step ? s.row_step * (4 / heads) : kStep;
     deal_out(few_, s.wgs * heads / s.H, s.least / heads, s.B, &wg_items, &mixed);
     big_first = (int32_t)items.size();
     wg_big.clear();
+    step_ = s.big_step ? s.big_step : kStep;
     deal_out(big_, s.big_wgs / s.H, s.big_least, s.B, &wg_big, &big_mixed);
     cut_alike(s.B);
 
@@ -474,7 +487,8 @@ class BatchPlan {
     for (const Use& u : uses_)
       for (int32_t j = 0; j < u.tokens; j++) join[at[lists[u.list + j]]++] = u.part + j * G;
   }
-  static constexpr int32_t kStep = 128;  // keys that a workgroup takes at a time
+  static constexpr int32_t kStep = 128;  // keys that a workgroup takes at a time at most, and is cut to without drafts
+  int32_t step_ = kStep;
   static constexpr int64_t kMany = 1024;  // keys of one head a workgroup
 
   // Does a tile without keys have something to do?  Only where its rows have no keys at any node.
@@ -491,10 +505,20 @@ class BatchPlan {
   }
   int64_t most_keys(int32_t B) const { return std::min<int64_t>((int64_t)(kMaxEntries - 1) * B, INT32_MAX / 2) / kStep * kStep; }
 
+  // Are keys that this node's requests share to be weighed as precisely as in row tiles?  With drafts only if one of these has few rows: those that
+  // have many weigh their own keys, and would weigh these without the others, as big tiles do.
+  bool fine(const Node& node) const {
+    if (node.reqs.size() < 2) return false;
+    if (tree.empty()) return true;
+    for (int32_t i : node.reqs)
+      if ((int64_t)q_len[i] * G <= row_tile_) return true;
+    return false;
+  }
+
   void add(const Tile& t, int32_t k0, int32_t k1, int32_t part, bool* any_mixed) {
     const int32_t end = std::max(k0, std::min(k1, t.limit));
     items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part,
-                     t.score, t.score_row, nodes_[t.node].from, nodes_[t.node].reqs.size() > 1});
+                     t.score, t.score_row, nodes_[t.node].from, t.fine});
     if (items.back().clear < end) *any_mixed = true;
   }
   int32_t take_rows(const Tile& t, int32_t rows) {
@@ -538,7 +562,7 @@ class BatchPlan {
     held = std::max<int64_t>(1, held);
     const int64_t most = most_keys(B);
     int64_t share = std::max<int64_t>(least, (work + held - 1) / held);
-    share = std::min(most, (share + kStep - 1) / kStep * kStep);
+    share = std::min(most, (share + step_ - 1) / step_ * step_);
     int64_t longest = 0, pieces = 0;
     auto count = [&] {
       pieces = 0;
@@ -551,18 +575,39 @@ class BatchPlan {
       count();
     }
     const bool line = pieces > held;
+    if (line && step_ != kStep) {
+      // with small steps the shares are nearly even, and a workgroup more than are to run at a time would come after all others
+      for (auto wgs_of = [&] {
+             int64_t count = 0, left = 0;
+             for (const Tile& t : tiles) {
+               if (idle(t)) continue;
+               int64_t keys = keys_of(t);
+               if (keys == 0 || left < step_) count++, left = share;
+               while (keys > 0) {
+                 int64_t n = std::min(keys, left);
+                 if (keys - n < step_ / 2 && keys <= most) n = keys;
+                 keys -= n;
+                 left -= (n + step_ - 1) / step_ * step_;
+                 if (keys > 0) count++, left = share;
+               }
+             }
+             return count;
+           };
+           share < most && wgs_of() > held;)
+        share += step_;
+    }
     int64_t room = 0;  // keys that the current workgroup still takes
     for (const Tile& t : tiles) {
       if (idle(t)) continue;
       const int32_t from = nodes_[t.node].from, keys = std::max(t.limit - from, 0);
       const bool whole_alone = alone(t);
-      if (!line || keys == 0 || room < kStep) {
+      if (!line || keys == 0 || room < step_) {
         wgs->push_back((int32_t)items.size());
         room = share;
       }
       if (!line) {  // equal pieces
         const int32_t n = (int32_t)std::max<int64_t>(1, (keys + share - 1) / share);
-        const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + kStep - 1) / kStep * kStep);
+        const int32_t step = (int32_t)(((int64_t)(keys + n - 1) / n + step_ - 1) / step_ * step_);
         for (int32_t c = 0; c < n && (c == 0 || (int64_t)c * step < keys); c++) {
           if (c) wgs->push_back((int32_t)items.size());
           const int32_t part = n == 1 && whole_alone ? -1 : take_rows(t, t.rows);
@@ -573,11 +618,11 @@ class BatchPlan {
       // a rest below half a step is taken along rather than left to another workgroup
       for (int32_t k = 0; k < keys || keys == 0;) {
         int32_t n = (int32_t)std::min<int64_t>(keys - k, room);
-        if (keys - k - n < kStep / 2 && keys - k <= most) n = keys - k;
+        if (keys - k - n < step_ / 2 && keys - k <= most) n = keys - k;
         const int32_t part = n == keys && whole_alone ? -1 : take_rows(t, t.rows);
         add(t, from + k, from + k + n, part, any_mixed);
         k += n;
-        room -= (n + kStep - 1) / kStep * kStep;
+        room -= (n + step_ - 1) / step_ * step_;
         if (keys == 0) break;
         if (k < keys) {
           wgs->push_back((int32_t)items.size());

@@ -47,6 +47,9 @@ int main(int argc, char** argv) {
     s.big_wgs = pick(0, 1) ? 512 : pick(1, 64);
     s.least = pick(0, 1) ? 512 : 128;
     s.big_least = pick(0, 1) ? 512 : 128;
+    s.row_tile = pick(0, 1) ? 32 : 16;
+    s.row_step = pick(0, 1) ? 32 : 0;
+    s.big_step = pick(0, 1) ? 64 : 0;
     const int n = pick(1, 8);
     std::vector<int32_t> off{0}, ids, len, ql;
     std::vector<uint8_t> trees;
@@ -122,7 +125,8 @@ int main(int argc, char** argv) {
           const bool may = x < limit[tok];
           bool bit = true;
           if (sight.word >= 0 && x >= sight.origin) {
-            CHECK((x - (x - it.k0) % 32 - sight.origin) % 32 == 0, "a step of 32 keys does not begin with a word");
+            const int step = big ? 64 : 32;
+            CHECK((x - (x - it.k0) % step - sight.origin) % step == 0, "a step does not begin with a word");
             const size_t at = (size_t)sight.word + (x - sight.origin) / 32;
             CHECK(at < bits.size(), "word %zu of %zu", at, bits.size());
             bit = bits[at] >> ((x - sight.origin) % 32) & 1;
