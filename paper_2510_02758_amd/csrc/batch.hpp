@@ -70,6 +70,8 @@ struct BatchShape {
   // Batches with drafts: rows of a row tile at most; keys that a workgroup takes at a time, by what it is cut to (0: kStep).
   int row_tile = 16;
   int row_step = 0, big_step = 0;
+  int most_heads = 4;  // of a workgroup of row tiles
+  int64_t cached_keys = 0;  // of all heads that the chip's last cache (256 MB) keeps
   int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
   // A prefix is shared from so many tokens on, by rows of one row tile and by more rows; the latter if all of them together spare `spared` tokens.
   int few_prefix = 64, big_prefix = 64;
@@ -91,6 +93,10 @@ inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cu
     s.row_tile = 32;
     s.row_step = 32;
     s.big_step = 64;
+    // Half a KB of neighbouring bytes is enough, and fewer heads mean longer runs of keys, so fewer pieces to join: 64 requests of 512 to 4096 tokens, eight
+    // drafts each, 8 heads of 128 in bf16, 139 us with two heads, 142 with four, 158 with one; 32 of 256 to 8192 with 32 drafts and 32 heads in fp8
+    // 261 with four, 278 with two, 294 with one.
+    s.most_heads = std::max(1, std::min(4, 512 / (D * (fp8 ? 1 : 2))));
   }
   s.H = H;
   s.B = B;
@@ -110,6 +116,7 @@ inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cu
   s.big_prefix = 1024;
   s.spared = (int64_t)230000000 / (2 * (int64_t)H * D * (fp8 ? 1 : 2));
   s.big_tile = big_tile(D);
+  s.cached_keys = (int64_t)200000000 / (2 * (int64_t)H * D * (fp8 ? 1 : 2));
   return s;
 }
 
@@ -307,6 +314,18 @@ class BatchPlan {
 
   std::vector<Node> nodes_;
 
+  // With drafts a request may have rows enough for tiles of its own.  Sharing a prefix then spares no products, and reads that come from the chip's caches
+  // anyway, but its partial results have to be joined.  Shared / not, us, 8 heads of 128 in bf16, requests of 40 to 900 tokens of their own: 48 with 128
+  // rows behind 2048 127 / 99, behind 4096 199 / 157, behind 8192 346 / 256; 24 with 128 behind 16384 330 / 246; 48 with 192 behind 4096 264 / 227; 48
+  // with 96 154 / 149; 64 with 68 152 / 149; 96 with 72 behind 2048 165 / 147; 32 with 160 behind 4096 158 / 159.  With 64 rows and fewer it is worth it: in
+  // fp8 with 40 behind 4096 121 / 158.
+  bool worth_sharing(const std::vector<int32_t>& reqs, int64_t keys, const BatchShape& s) const {
+    if (tree.empty() || keys > s.cached_keys) return true;
+    for (int32_t i : reqs)
+      if ((int64_t)q_len[i] * G <= s.big_tile / 2) return true;
+    return false;
+  }
+
   // -> tokens that big tiles do not read again.
   int64_t find_nodes(const BatchShape& s, bool share_big) {
     const int32_t B = s.B;
@@ -342,7 +361,7 @@ class BatchPlan {
         const int64_t keys = (int64_t)(at - w.from) * B;
         int64_t rows = 0;
         for (int32_t i : w.reqs) rows += (int64_t)q_len[i] * G;
-        if (rows <= s.row_tile ? keys >= s.few_prefix : share_big && keys >= s.big_prefix) {
+        if (rows <= s.row_tile ? keys >= s.few_prefix : share_big && keys >= s.big_prefix && worth_sharing(w.reqs, keys, s)) {
           nodes_.push_back({w.reqs, w.from * B, at * B});
           w.from = at;
           if (rows > s.row_tile) spared += keys * (int64_t)(w.reqs.size() - 1);
@@ -467,6 +486,7 @@ class BatchPlan {
     // than four runs of one head's keys: they then read neighbouring bytes at the same time.  64 requests of 512 to 4096 tokens with 8
     // heads of 128 in bf16: 103 us instead of 135, 32 requests of 256 to 8192 with 32 heads in fp8: 175 to 181 instead of 207.
     heads = work * s.H / std::max(1, s.wgs) < kMany ? 1 : s.H % 4 == 0 ? 4 : s.H % 2 == 0 ? 2 : 1;
+    if (!tree.empty()) heads = std::min(heads, s.most_heads);
     wg_items.clear();
     step_ = s.row_step ? s.row_step * (4 / heads) : kStep;
     deal_out(few_, s.wgs * heads / s.H, s.least / heads, s.B, &wg_items, &mixed);
