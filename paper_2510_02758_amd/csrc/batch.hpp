@@ -32,6 +32,8 @@ struct AttnItem {
   // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
   int32_t score, score_row, score_from;
   int32_t fine;  // keys that several requests share.  In big tiles their weights are as precise as in row tiles, whatever these requests' number
+  // Of a drafted tree (TreeReq): where the bits of row tree_first begin (-1: no tree's keys), words of a row, their first key.
+  int32_t tree, tree_first, tree_words, tree_origin;
 };
 // One piece of weight accumulation whose products are computed again: keys [k0, k1) that `count` requests have in common, for the
 // rows of these, requests wreqs[first ..].
@@ -306,6 +308,11 @@ class BatchPlan {
       tree_units = std::max(tree_units, r.rows * std::max(r.words, 1));
       for (int32_t j = 0; j < r.rows; j++) tree_sight.push_back({r.words ? r.word + j * r.words : -1, r.origin});
     }
+    for (AttnItem& it : items) {
+      if (it.clear >= it.k1) continue;  // (all of its keys are seen by all rows)
+      const TreeReq& r = tree_reqs[tok_req[lists[it.tokens]]];
+      if (r.words) it.tree = r.word, it.tree_first = r.first, it.tree_words = r.words, it.tree_origin = r.origin;
+    }
     tree_tails_shared = twice([&](auto what) {
       for (int32_t i = 0; i < n; i++)
         if (tree[i] && q_len[i] > 1) what(off[i] + (len[i] - q_len[i]) / B, off[i] + (int32_t)(((int64_t)len[i] + B - 1) / B));
@@ -538,7 +545,7 @@ class BatchPlan {
   void add(const Tile& t, int32_t k0, int32_t k1, int32_t part, bool* any_mixed) {
     const int32_t end = std::max(k0, std::min(k1, t.limit));
     items.push_back({off[nodes_[t.node].reqs[0]], k0, end, std::min(end, t.clear), t.list, t.row0, t.rows, part,
-                     t.score, t.score_row, nodes_[t.node].from, t.fine});
+                     t.score, t.score_row, nodes_[t.node].from, t.fine, -1, 0, 0, 0});
     if (items.back().clear < end) *any_mixed = true;
   }
   int32_t take_rows(const Tile& t, int32_t rows) {

@@ -119,7 +119,8 @@ int main(int argc, char** argv) {
       CHECK(it.clear >= it.k1 || (big ? p.big_mixed : p.mixed), "mixed");
       for (int r = it.row0; r < it.row0 + it.rows; r++) {
         const int tok = p.lists[it.tokens + r / G], row = tok * G + r % G, req = p.tok_req[tok];
-        const kvswap::TreeSight sight = p.tree_sight[tok];
+        const kvswap::TreeSight sight = it.tree < 0 ? kvswap::TreeSight{-1, 0} : kvswap::TreeSight{it.tree + (tok - it.tree_first) * it.tree_words, it.tree_origin};
+        CHECK(it.tree < 0 || (sight.word == p.tree_sight[tok].word && sight.origin == p.tree_sight[tok].origin), "where the bits of row %d are", tok);
         for (int x = it.k0; x < it.k1; x++) {
           CHECK(p.ids[it.table + x / s.B] == ids[off[req] + x / s.B], "block of key %d", x);
           const bool may = x < limit[tok];
