@@ -1,6 +1,6 @@
 // C ABI of the operators on the pool's contents (declared in include/kvswap.h): the batch, rotary append, attention, eviction, accepted drafts.
-// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append and kv_accept, two for kv_evict (one and two
-// for each part of their layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
+// Host side of each call: check everything, then a few launches on the caller's stream: one for kv_append and kv_accept, two for kv_evict (two for
+// each part of its layers where all of them need more workgroups than a launch can have), for kv_attn one or two for the tiles, one for their join
 // and up to two for the weights.  Nothing waits on the host outside kv_batch_create, kv_batch_set and kv_batch_destroy, and nothing is
 // allocated there but the first room for kept products and for the order of moves, when they are first needed.
 #include <hip/hip_runtime.h>
@@ -536,13 +536,18 @@ int append(kv_batch* b, const kv_append_args* a, int32_t axes, const int32_t* pa
     k.units = k.pairs + (v.D - a->rot) / 8;
     k.chunks = ((k.Hq + v.H) * k.units + v.H * (v.D / 8) + 255) / 256;
   }
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)pl.T * (wide ? k.chunks : 1)), dim3(256), 0, st, k); };
+  k.T = pl.T;
+  auto go = [&](auto kern, int64_t wgs) { hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 0, st, k); };
+  const int64_t all = (int64_t)pl.T * k.chunks;
   auto any = [&](auto e, auto p, auto x) {
     using E = decltype(e);
-    if (wide)
-      go(kv_append_wide_kernel<E, decltype(p)::value, decltype(x)::value>);
+    constexpr bool P = decltype(p)::value, X = decltype(x)::value;
+    if (!wide)
+      go(kv_append_kernel<E, P, X>, pl.T);
+    else if (all <= kAppendMany * v.cus)
+      go(kv_append_wide_kernel<E, P, X, 1>, all);
     else
-      go(kv_append_kernel<E, decltype(p)::value, decltype(x)::value>);
+      go(kv_append_wide_kernel<E, P, X, 2>, (int64_t)(pl.T + 1) / 2 * k.chunks);
   };
   auto typed = [&](auto p, auto x) { f16 ? any(_Float16(), p, x) : any(__bf16(), p, x); };
   auto stored = [&](auto x) { fp8 ? typed(std::true_type(), x) : typed(std::false_type(), x); };
@@ -774,7 +779,7 @@ int kv_accept(kv_batch* b, const kv_accept_args* a, void* stream) try {
   AcceptArgs k{};
   k.cols = (bytes / vec + 255) / 256;
   k.vecs = (bytes / vec + k.cols - 1) / k.cols;
-  if ((int64_t)pl.n * 2 * k.cols > kMostWgs) return KV_EINVAL;
+  if ((int64_t)pl.n * k.cols > kMostWgs) return KV_EINVAL;
   std::vector<int32_t> unchanged;
   if (a->req_ids) {
     if (!v.plan_only && is_capturing((hipStream_t)stream)) return KV_EINVAL;
@@ -815,23 +820,24 @@ int kv_accept(kv_batch* b, const kv_accept_args* a, void* stream) try {
     k.head = v.D * elem(v);
     k.weights = a->weights;
     for (int i = 0; i < 3; i++) k.ws[i] = a->weights_strides[i];
-    // as many layers at a time as one launch may have workgroups for; without trees, or without layers, the counts alone
-    const int64_t layer_wgs = (int64_t)pl.n * 2 * k.cols;
-    const int32_t most = (int32_t)std::min<int64_t>(v.L, std::max<int64_t>(1, kMostWgs / layer_wgs)), all = trees ? a->num_layers : 0;
-    for (int32_t done = 0; done == 0 || done < all; done += most) {
-      k.layers = std::min(most, all - done);
-      const unsigned wgs = k.layers ? (unsigned)(k.layers * layer_wgs) : (unsigned)(pl.n * k.cols);
-      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(wgs), dim3(256), 0, st, k); };
-      if (v.scale)
-        vec == 16 ? go(kv_accept_kernel<u32x4, true>) : go(kv_accept_kernel<u32x2, true>);
-      else
-        vec == 16 ? go(kv_accept_kernel<u32x4, false>) : go(kv_accept_kernel<u32x2, false>);
-      OPCHK(b, hipGetLastError());
-      k.count = nullptr;  // (told by the first)
-      k.pool += most * k.ls;
-      if (k.scale) k.scale += most * k.sls;
-      if (k.weights) k.weights += most * k.ws[0];
-    }
+    k.layers = trees ? a->num_layers : 0;
+    // as many workgroups as fit the chip at a time (8 a CU) share the planes; without trees, or without layers, the counts alone
+    const int64_t each = (int64_t)pl.n * k.cols;
+    k.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(2 * k.layers, 8 * v.cus / each));
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(each * k.groups)), dim3(256), 0, st, k); };
+    // a workgroup that has one plane takes eight rows of it at a time, one that has more four of two
+    auto any = [&](auto scaled, auto q) {
+      constexpr bool S = decltype(scaled)::value;
+      constexpr int Q = decltype(q)::value;
+      vec == 16 ? go(kv_accept_kernel<u32x4, S, Q>) : go(kv_accept_kernel<u32x2, S, Q>);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    if (k.groups >= 2 * k.layers)
+      v.scale ? any(std::true_type(), one) : any(std::false_type(), one);
+    else
+      v.scale ? any(std::true_type(), two) : any(std::false_type(), two);
+    OPCHK(b, hipGetLastError());
   }
   if (a->req_ids) kvswap::pool_rewritten(b->pool, pl.n, a->req_ids, unchanged.data());
   return KV_OK;

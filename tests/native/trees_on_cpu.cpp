@@ -232,14 +232,18 @@ int main(int argc, char** argv) {
     a.vk = plane;
     a.bs = block;
     a.row = row;
+    a.groups = pick(1, 2 * layers);
     a.cols = (row / vec + 255) / 256;
     a.vecs = (row / vec + a.cols - 1) / a.cols;
     a.weights = weights.data();
     a.ws[0] = cap * s.H * n;
     a.ws[1] = cap * s.H;
     a.ws[2] = cap;
-    auto run = [&](auto kern) { mockhip::run_grid(dim3((unsigned)(layers * 2 * n * a.cols)), dim3(256), 16, [&] { kern(a); }); };
-    vec == 16 ? run(kv_accept_kernel<u32x4, false>) : run(kv_accept_kernel<u32x2, false>);
+    auto run = [&](auto kern) { mockhip::run_grid(dim3((unsigned)(a.groups * n * a.cols)), dim3(256), 16, [&] { kern(a); }); };
+    if (pick(0, 1))
+      vec == 16 ? run(kv_accept_kernel<u32x4, false, 1>) : run(kv_accept_kernel<u32x2, false, 1>);
+    else
+      vec == 16 ? run(kv_accept_kernel<u32x4, false, 2>) : run(kv_accept_kernel<u32x2, false, 2>);
     for (int i = 0; i < n; i++) CHECK(count[i] == wcount[i] && next[i] == wnext[i], "request %d: %d rows, then %d, instead of %d, %d", i, count[i], next[i], wcount[i], wnext[i]);
     CHECK(pool == want, "the pool");
     CHECK(weights == wwant, "the weights");
