@@ -58,6 +58,7 @@ TREES = {
     "d 256, blocks of 16": ((2, 2, 256, 16, "bf16", False), 4, [300, 77], [4, 70], ["random", "strange"], (), "layer", (0, 0)),
     "d 8": ((1, 2, 8, 8, "bf16", False), 2, [70], [9], ["random"], (), "layer", (0, 0)),
     "many query heads": ((1, 1, 128, 16, "bf16", False), 71, [290, 45], [3, 2], ["star", "padded"], (), "layer", (0, 0)),
+    "more query heads than a tile has rows": ((1, 1, 64, 16, "bf16", False), 150, [290, 45, 30], [3, 2, 4], ["star", "padded", "-"], (), "layer", (0, 0)),
     "long, few rows": ((1, 1, 128, 16, "bf16", False), 2, [20011], [8], ["random"], (), "layer", (0, 0)),
     "long, many rows": ((1, 1, 128, 16, "bf16", False), 8, [20011], [48], ["random"], (), "layer", (0, 0)),
     "long, token by token": ((1, 1, 64, 1, "f16", False), 4, [9001], [13], ["random"], (), "layer", (0, 0)),
@@ -137,6 +138,78 @@ def test_tree_attention(gpu, name):
             slack = (2.0 ** -22 * (1 + np.abs(rw[i])) + wtol[i]) * (1 + q_lens[i])
             assert (np.abs(added - rw[i]) <= slack).all(), i
             assert torch.equal(weights[i, :, n:], start[i, :, n:])
+
+
+@pytest.mark.parametrize("name", ["few rows", "32 rows", "fp8 with scales", "behind a prefix"])
+def test_captured_weights(gpu, name):
+    """The first call that wants weights is in a capture: there is no room for products, which are computed again."""
+    import torch
+    (L, H, D, B, dtype, _), G, lens, q_lens, *_ = TREES[name]
+    p, rows, trees, parents = _drafts(gpu, name)
+    o, ids = R.csr(rows)
+    io_name = "f16" if dtype == "f16" else "bf16"
+    q = torch.from_numpy(p.rng.standard_normal((sum(q_lens), G * H, D)) * (1.0 if dtype != "fp8_e4m3" else 0.1)).to(_torch_type(io_name)).to(gpu)
+    ref, tol, _, _, rw, wtol = TR.attention(p.values()[L - 1], rows, lens, q_lens, trees, q.double().cpu().numpy(), D ** -0.5, io_name, B)
+    _spoil_rows_of_no_tree(p, rows, lens, q_lens, trees, q)
+    out, weights = torch.empty_like(q), torch.zeros(len(lens), H, max(lens), device=gpu)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    kv.kv_check(p.batch.set_trees(o, ids, lens, q_lens, G * H, parents, [t is not None for t in trees], stream=st))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        kv.kv_check(p.batch.attn(L - 1, q, out, D ** -0.5, weights=weights, stream=st))
+    for turn in range(3):
+        weights.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            graph.replay()
+        st.synchronize()
+        assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
+        for i, n in enumerate(lens):
+            assert (np.abs(weights[i, :, :n].double().cpu().numpy() - rw[i]) <= (2.0 ** -22 * (1 + np.abs(rw[i])) + wtol[i]) * (1 + q_lens[i])).all(), (turn, i)
+
+
+def test_far_into_a_pool(gpu):
+    """Blocks whose bytes lie beyond 4 GiB from the layer's first: what is appended, seen and moved there."""
+    import torch
+    g = W.Geometry(1, 8, 128, 16, "bf16", 150000)
+    raw = torch.empty(g.pool_bytes, dtype=torch.uint8, device=gpu)
+    arena = torch.empty(g.S, dtype=torch.uint8, device=gpu)
+    kp = kv.KVPool(g, raw, arena, flags=kv.KV_STAGING_DEVICE)
+    b = kv.KVBatch(kp)
+    view = raw.view(torch.bfloat16).view(1, 2, g.N, g.B, g.H, g.D)
+    rng = np.random.default_rng(0)
+    rows = [np.array([149999, 3, 149998, 140000, 139999], np.int32), np.array([131072, 131071, 149000], np.int32)]
+    lens, q_lens, G = [77, 40], [20, 9], 4
+    every = torch.from_numpy(np.concatenate(rows)).long().to(gpu)
+    view[0, :, every] = torch.randn(2, 8, g.B, g.H, g.D, device=gpu).bfloat16()
+    trees = [_parents(rng, n, "random") for n in q_lens]
+    parents = torch.tensor(sum(trees, []), dtype=torch.int32, device=gpu)
+    o, ids = R.csr(rows)
+    kv.kv_check(b.set_trees(o, ids, lens, q_lens, G * 8, parents))
+    k, v = (torch.randn(29, 8, 128, device=gpu).bfloat16() for _ in range(2))
+    kv.kv_check(b.append(0, None, k, v))
+    q = torch.randn(29, G * 8, 128, device=gpu).bfloat16()
+    out = torch.empty_like(q)
+    kv.kv_check(b.attn(0, q, out, 128 ** -0.5))
+    small = view[0][:, every].double().cpu().numpy()
+    at = [np.arange(5), np.arange(5, 8)]
+    ref, tol, *_ = TR.attention(small, at, lens, q_lens, trees, q.double().cpu().numpy(), 128 ** -0.5, "bf16", 16)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
+    tokens, chosen = _answers(rng, trees, q_lens, [5, 4])
+    dev = lambda x: torch.from_numpy(x.astype(np.int32)).to(gpu)  # noqa: E731
+    count, nxt, path = dev(np.zeros(2)), dev(np.zeros(2)), dev(np.zeros((2, 20)))
+    kv.kv_check(b.accept(0, 1, dev(tokens), dev(chosen), count, path, nxt))
+    after = view[0][:, every].double().cpu().numpy()
+    t = 0
+    for i, (tree, n, new) in enumerate(zip(trees, lens, q_lens)):
+        way, follows = TR.accepted(tree, tokens[t:t + new], chosen[t:t + new])
+        t += new
+        assert count[i] == len(way) > 1 and nxt[i] == follows
+        x = np.concatenate([np.arange(n - new), n - new + np.array(way)])
+        y = np.arange(n - new + len(way))
+        assert np.array_equal(after[:, at[i][y // 16], y % 16], small[:, at[i][x // 16], x % 16])
 
 
 def test_a_chain_is_a_prompt(gpu):
@@ -583,3 +656,12 @@ def test_the_same_bits_twice(gpu):
         got.append((out.view(torch.int16), lse.view(torch.int32), w.view(torch.int32)))
     for x in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(x, got[0]))
+
+
+def test_the_drafting_example(gpu):
+    """Prompts with images, drafts, attention over their trees, and accepted paths in one loop: what it leaves in the cache and answers is what the same
+    tokens give one at a time, 16-bit roundings apart."""
+    from paper_2510_02758_amd import stream_demo
+    r = stream_demo.speculate()
+    assert r["accepted"] > 1 and r["tokens"] >= 20
+    assert r["hidden"] < 0.05 and r["cache"] < 0.05

@@ -29,6 +29,23 @@ def test_plan_and_kernels_against_plain_loops(tmp_path):
     assert r.returncode == 0 and "trees ok" in r.stdout, r.stdout + r.stderr
 
 
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    if not os.path.exists(CLANGXX):
+        pytest.skip("no host clang++ for the kernel source")
+    exe, mock = str(tmp_path_factory.mktemp("trees") / "trees_host"), os.path.join(HERE, "native", "mockhip")
+    subprocess.check_call([CLANGXX, "-std=c++17", "-O1", "-g", "-pthread", "-Wno-unused-function", "-Wno-keyword-macro", "-fsanitize=address,undefined",
+                           "-fno-sanitize-recover=all", "-I", mock, "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2510_02758_amd", "csrc"),
+                           "-I", os.path.join(HERE, "native"), "-o", exe, os.path.join(HERE, "native", "trees_host_on_mock_hip.cpp"), os.path.join(mock, "mockhip.cpp")])
+    return exe
+
+
+@pytest.mark.parametrize("name", ["trees_of_a_batch", "captures_and_replays", "launches_of_an_acceptance", "launches_of_large_trees"])
+def test_host_side(host, name):
+    r = subprocess.run([host, name], capture_output=True, text=True, timeout=120, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:detect_stack_use_after_return=0"))
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
 def test_the_oracle_notices_mistakes():
     """What the plain implementation says of a small tree, by hand; a planted mistake would differ."""
     #        0 - 1 - 3          2 hangs on 0, 4 on 2; 5 is in no tree, nor is 6, which hangs on it; 7 is a root of its own
