@@ -95,6 +95,11 @@ inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cu
     s.row_tile = 32;
     s.row_step = 32;
     s.big_step = 64;
+    // A step of drafts is short, and its join costs half of what kv_attn_join_kernel takes, so it is cut finer than a prompt.  Cut from 512 keys on / from
+    // 256 on, one request with 64 drafts of 1000 tokens 25.7 / 22.1 us, of 4000 30.1 / 28.7, with 16 of 2000 19.6 / 16.8.  Partial rows that cost as much as
+    // a key, 50 / 100 in bf16: 16 requests of 500 to 2000 with 16 drafts 43 / 32, 40 of 1000 to 4000 with 32 145 / 130, 60 of 3000 to 4000 with 16 and 8
+    // query heads each 192 / 191 (200: 227); 100 / 200 in fp8: 16 of 1000 to 4000 with 48 133 / 122, 4 of 1000 with 64 36 / 30.
+    s.big_least = 256;
     // Half a KB of neighbouring bytes is enough, and fewer heads mean longer runs of keys, so fewer pieces to join: 64 requests of 512 to 4096 tokens, eight
     // drafts each, 8 heads of 128 in bf16, 139 us with two heads, 142 with four, 158 with one; 32 of 256 to 8192 with 32 drafts and 32 heads in fp8
     // 261 with four, 278 with two, 294 with one.
@@ -106,7 +111,7 @@ inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cu
   s.wgs = cus * 2;
   s.big_cu = D <= 128 ? 2 : 1;
   s.big_wgs = cus * s.big_cu;
-  s.key_rows = fp8 ? 100 : 50;
+  s.key_rows = (fp8 ? 100 : 50) * (s.big_step ? 2 : 1);
   // Sharing a prefix costs a join of partial results (3 to 5 us), and for more than 16 rows big tiles, which take 25 us (fp8: 30) however little there is
   // to do; and repeated reads of a short prefix come from the caches.  Decode steps, 8 heads of 128 with 4 query heads each, prefix shared / read by each
   // request, bf16 us, then fp8.  Up to 16 rows: 2 requests behind 256 tokens 11.5 / 9.7, 11.0 / 8.6, behind 1024 13.2 / 12.4, 13.2 / 12.3; 32 pairs
