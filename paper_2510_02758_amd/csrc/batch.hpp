@@ -92,7 +92,8 @@ constexpr bool whole_rows(int D, int B) { return (D == 64 || D == 128 || D == 25
 inline BatchShape batch_shape(int32_t H, int32_t D, int32_t B, int64_t N, int cus, bool fp8, bool trees = false) {
   BatchShape s;
   if (trees && whole_rows(D, B)) {
-    s.row_tile = 32;
+    // (two 16s of rows of 256 elements have no room in a wavefront's registers)
+    s.row_tile = D <= 128 ? 32 : 16;
     s.row_step = 32;
     s.big_step = 64;
     // A step of drafts is short, and its join costs half of what kv_attn_join_kernel takes, so it is cut finer than a prompt.  Cut from 512 keys on / from
