@@ -80,6 +80,13 @@ struct JoinArgs {
   const int32_t* limit;  // of a batch with drafted trees: 0 is a row that is in none
 };
 
+// kv_attn_join_few_kernel: lanes of a row, workgroups of a token, and of a launch (0: it would have more lanes than 32 bits count).
+constexpr int join_few_stride(int D) { return D <= 64 ? 16 : D <= 128 ? 32 : 64; }
+constexpr int64_t join_few_chunks(int64_t heads, int D) { return (heads * join_few_stride(D) + 255) / 256; }
+constexpr int64_t join_few_wgs(int64_t T, int64_t heads, int D) {
+  return T * join_few_chunks(heads, D) <= UINT32_MAX / 256 ? T * join_few_chunks(heads, D) : 0;
+}
+
 struct WeightArgs {
   AttnArgs a;
   const kvswap::WeightItem* items;

@@ -296,7 +296,8 @@ int set_batch(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* blo
     pl.n = pl.T = 0;
     return rc;
   }
-  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads, kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3, trees != nullptr), trees);
+  rc = pl.set(n, offsets, block_ids, num_tokens, q_lens, num_q_heads,
+              kvswap::batch_shape(b->v.H, b->v.D, b->v.B, b->v.N, b->v.cus, b->v.dtype == KV_FP8_E4M3, trees != nullptr), trees);
   if (rc) return rc;
   b->max_len = b->max_tree = 0;
   for (int32_t i = 0; i < pl.n; i++) b->max_len = std::max(b->max_len, pl.len[i]);
@@ -319,9 +320,11 @@ int set_batch(kv_batch* b, int32_t n, const int32_t* offsets, const int32_t* blo
     const void** at;
   };
 #define VEC(x, to) Part{(x).data(), (x).size() * sizeof((x)[0]), (const void**)&(to)}
-  const Part parts[] = {VEC(pl.items, b->items),   VEC(pl.wg_items, b->wg_items), VEC(pl.wg_big, b->wg_big), VEC(pl.witems, b->witems), VEC(pl.wrest, b->wrest), VEC(pl.sitems, b->sitems), VEC(pl.wreqs, b->wreqs),     VEC(pl.ids, b->table),    VEC(pl.off, b->off),
-                        VEC(pl.len, b->len),       VEC(pl.q_first, b->q_first),   VEC(pl.places, b->places), VEC(pl.tok_limit, b->limit),
-                        VEC(pl.lists, b->lists),   VEC(pl.join_off, b->join_off), VEC(pl.join, b->join), VEC(pl.tree_reqs, b->tree_reqs), VEC(pl.tree_sight, b->tree_sight)};
+  const Part parts[] = {VEC(pl.items, b->items),     VEC(pl.wg_items, b->wg_items),   VEC(pl.wg_big, b->wg_big),       VEC(pl.witems, b->witems),
+                        VEC(pl.wrest, b->wrest),     VEC(pl.sitems, b->sitems),       VEC(pl.wreqs, b->wreqs),         VEC(pl.ids, b->table),
+                        VEC(pl.off, b->off),         VEC(pl.len, b->len),             VEC(pl.q_first, b->q_first),     VEC(pl.places, b->places),
+                        VEC(pl.tok_limit, b->limit), VEC(pl.lists, b->lists),         VEC(pl.join_off, b->join_off),   VEC(pl.join, b->join),
+                        VEC(pl.tree_reqs, b->tree_reqs), VEC(pl.tree_sight, b->tree_sight)};
 #undef VEC
   size_t need = 0;
   for (const Part& p : parts) need += padded(p.bytes);

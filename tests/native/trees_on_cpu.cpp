@@ -248,6 +248,15 @@ int main(int argc, char** argv) {
     CHECK(pool == want, "the pool");
     CHECK(weights == wwant, "the weights");
   }
+  // the join's launch: a row of its own lanes for every head of every token, and never more lanes than 32 bits count
+  for (int64_t T : {1ll, 1000ll, 16777215ll, 16777216ll, 20000000ll, 500000000ll})
+    for (int heads : {1, 3, 8, 64, 128})
+      for (int D : {8, 64, 72, 128, 136, 256}) {
+        const int seed = -1;  // (none)
+        const int64_t wgs = join_few_wgs(T, heads, D);
+        CHECK(wgs * 256 <= UINT32_MAX, "%ld tokens of %d heads of %d: %ld workgroups", (long)T, heads, D, (long)wgs);
+        if (T <= 1000) CHECK(wgs == T * join_few_chunks(heads, D) && wgs * 256 >= T * heads * join_few_stride(D) && join_few_stride(D) * 4 >= D, "%ld workgroups", (long)wgs);
+      }
   if (!masked_pairs || !moved || !shared_seen || !refused) return fprintf(stderr, "nothing was looked at: %ld %ld %ld %ld\n", masked_pairs, moved, shared_seen, refused), 1;
   printf("trees ok\n");
   return 0;
