@@ -423,12 +423,13 @@ const char* kv_strerror(int code);
  * table[index / B] at place index % B.  Tables are CSR as in kv_swap_out; a row may be longer than the tokens need.
  * A request with num_tokens 0 may still have one row (a padded batch): nothing is stored for it and it sees nothing.
  * Requests whose tables begin with the same blocks share these: kv_attn reads such a prefix once for all of them where that is faster, which is
- * from 512 tokens on for up to 16 rows of a KV head, and for more from 1024 on if it spares the step 230 MB a layer. */
+ * from 512 tokens on for up to 16 rows of a KV head (new tokens times query heads; 32 where requests draft), and for more from 1024 on if it spares the
+ * step 230 MB a layer.  Requests that draft do without if each of them has more than 64 rows (heads above 128: 32) and the prefix has up to 200 MB a layer. */
 typedef struct kv_batch kv_batch; /* opaque */
 
 /* A batch on the pool; the pool must outlive it (KV_EINVAL: a head_dim that is no multiple of 8, above 128 none of 16, or above 256).
- * The batch owns device memory for the tables, the plan of the attention and its partial results, which kv_batch_set allocates as
- * batches grow (it waits on the host for the batch's earlier work where it does).  Two more parts are allocated by the first call that wants them, and
+ * The batch owns device memory for the tables, the plan of the attention, its partial results and what drafted trees' rows see, which kv_batch_set
+ * allocates as batches grow (it waits on the host for the batch's earlier work where it does).  Two more parts are allocated by the first call that wants them, and
  * from then on by kv_batch_set.  One is kv_attn's with weights, for products: 4 bytes for each of a row tile's up to 16 rows and its keys.  Without
  * it, for want of memory or because the first such call is in a capture, they are computed twice.  The other is kv_evict's, for the order of its moves:
  * 8 bytes for each layer, head and some 128 tokens of the longest request, times n.  Without it, and always in a capture, each head's moves are made
@@ -533,7 +534,9 @@ int kv_append_axes(kv_batch* b, const kv_append_args* a, int32_t axes, const int
  * Arithmetic: products of io-type elements (fp8 ones widened exactly) accumulate in 32 bits; softmax statistics and sums are 32 bits; out is
  * rounded once.  For the product with V the weights go into 16 bits: in two terms, which leave out less than 2^-16 of each (in f16: or 2^-34 of
  * the row's largest), or in one, rounded to io_dtype as out is.  One term is for the tokens that a request has for itself where it has more than
- * 16 rows for a KV head (new tokens times query heads: a prompt); all else has two, whatever other requests are in the batch. */
+ * 16 rows for a KV head (new tokens times query heads: a prompt); all else has two, whatever other requests are in the batch.  In a batch with drafted
+ * trees it is for requests with more than 32 rows (16 where heads are not 64 or 128 elements, or blocks no multiple of 16 tokens), which then have one for a
+ * prefix, too, if all that share it have as many. */
 typedef struct {
   uint32_t struct_size;
   int32_t layer;
