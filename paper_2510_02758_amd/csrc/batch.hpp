@@ -609,13 +609,14 @@ class BatchPlan {
     }
     const bool line = pieces > held;
     if (line && step_ != kStep) {
-      // with small steps the shares are nearly even, and a workgroup more than are to run at a time would come after all others
+      // with small steps the shares are nearly even, and a workgroup more than are to run at a time would come after all others.  Tiles without keys
+      // (padded requests) do not count: each has a workgroup whatever the share is, which is soon over.
       for (auto wgs_of = [&] {
              int64_t count = 0, left = 0;
              for (const Tile& t : tiles) {
-               if (idle(t)) continue;
                int64_t keys = keys_of(t);
-               if (keys == 0 || left < step_) count++, left = share;
+               if (keys == 0) continue;
+               if (left < step_) count++, left = share;
                while (keys > 0) {
                  int64_t n = std::min(keys, left);
                  if (keys - n < step_ / 2 && keys <= most) n = keys;
