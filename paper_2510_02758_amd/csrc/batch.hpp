@@ -46,9 +46,10 @@ struct ScoreItem {
 };
 
 // A tree's request, for the kernel that finds out what its rows see.  A row has `words` words of 32 bits, an even number, for the keys from `origin` on
-// (what lies in front of it every row of the tree sees), the first of its request's rows at `word`.  words 0: the new tokens follow one another.
+// (what lies in front of it every row of the tree sees), the first of its request's rows at `word`.  words 0: the new tokens follow one another, or there
+// is nothing that they could see.  tree: the request drafts, also where words is 0 (a padded one).
 struct TreeReq {
-  int32_t first, rows, base, word, words, origin;
+  int32_t first, rows, base, word, words, origin, tree;
 };
 // The same as a row of the attention needs it; word -1: the row sees the keys in front of its limit.
 struct TreeSight {
@@ -303,7 +304,7 @@ class BatchPlan {
     for (const Node& node : nodes_)
       if (node.reqs.size() == 1 && node.to == len[node.reqs[0]]) from[node.reqs[0]] = node.from;
     for (int32_t i = 0; i < n; i++) {
-      TreeReq r{q_first[i], q_len[i], std::max(len[i] - q_len[i], 0), 0, 0, 0};
+      TreeReq r{q_first[i], q_len[i], std::max(len[i] - q_len[i], 0), 0, 0, 0, tree[i]};
       if (tree[i] && len[i] && q_len[i]) {
         r.origin = from[i] + (r.base - from[i]) / 64 * 64;
         r.words = (len[i] - r.origin + 63) / 64 * 2;

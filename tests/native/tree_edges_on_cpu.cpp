@@ -52,11 +52,54 @@ void weights_of_rows_that_see_nothing() {
   for (int x = 0; x < keys; x++) CHECK(std::fabs(weights[x] - want[x]) <= 1e-5f * want[x]);
 }
 
+// A padded batch: requests that draft, one that has nothing cached and one row, one without rows, and one whose new tokens are no tree.  What was in `path`
+// goes from every row of a tree, and from no other.
+void paths_of_padded_trees() {
+  kvswap::BatchShape s;
+  s.B = 4;
+  s.H = 1;
+  s.N = 64;
+  const int n = 5, most = 6;
+  const int32_t off[n + 1] = {0, 3, 3, 6, 9, 9}, ids[9] = {1, 2, 3, 4, 5, 6, 7, 8, 9}, len[n] = {10, 0, 9, 12, 0}, ql[n] = {4, 1, 0, 3, 1};
+  const uint8_t trees[n] = {1, 1, 1, 0, 1};
+  kvswap::BatchPlan p;
+  CHECK(p.set(n, off, ids, len, ql, 1, s, trees) == KV_OK && p.T == 9);
+  const int32_t parents[9] = {-1, 0, 1, -2, -1, 7, 7, 7, -2};
+  std::vector<int32_t> parent(9), position(9), limit = p.tok_limit, tokens(9, 5), chosen(9, 5), count(n, -9), next(n, -9), path((size_t)n * most, -9);
+  std::vector<uint32_t> bits((size_t)p.tree_words);
+  TreeArgs t{p.tree_reqs.data(), parents, (p.tree_units + 255) / 256, parent.data(), position.data(), limit.data(), bits.data()};
+  mockhip::run_grid(dim3((unsigned)(n * t.chunks)), dim3(256), 16, [&] { kv_tree_kernel(t); });
+  AcceptArgs a{};
+  a.reqs = p.tree_reqs.data();
+  a.parent = parent.data();
+  a.tokens = tokens.data();
+  a.chosen = chosen.data();
+  a.q_first = p.q_first.data();
+  a.len = p.len.data();
+  a.off = p.off.data();
+  a.table = p.ids.data();
+  a.count = count.data();
+  a.path = path.data();
+  a.next = next.data();
+  a.path_stride = most;
+  a.n = n;
+  a.H = 1;
+  a.B = s.B;
+  a.row = 16;
+  a.groups = a.cols = a.vecs = 1;
+  mockhip::run_grid(dim3((unsigned)n), dim3(256), 16, [&] { kv_accept_kernel<u32x4, false, 1>(a); });
+  CHECK((count == std::vector<int32_t>{3, 0, 0, 3, 0}) && (next == std::vector<int32_t>{5, -1, -1, 5, -1}));
+  const std::vector<int32_t> want[n] = {{0, 1, 2, -1, -9, -9}, {-1, -9, -9, -9, -9, -9}, {-9, -9, -9, -9, -9, -9}, {-9, -9, -9, -9, -9, -9}, {-1, -9, -9, -9, -9, -9}};
+  for (int i = 0; i < n; i++)
+    for (int k = 0; k < most; k++) CHECK(path[i * most + k] == want[i][k]);
+}
+
 }  // namespace
 
 int main(int, char** argv) {
   const std::string name = argv[1];
   if (name == "weights_of_rows_that_see_nothing") weights_of_rows_that_see_nothing();
+  else if (name == "paths_of_padded_trees") paths_of_padded_trees();
   else return 2;
   std::printf("ok\n");
   return 0;

@@ -33,7 +33,7 @@ def edges(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["weights_of_rows_that_see_nothing"])
+@pytest.mark.parametrize("name", ["weights_of_rows_that_see_nothing", "paths_of_padded_trees"])
 def test_kernels_at_their_edges(edges, name):
     r = subprocess.run([edges, name], capture_output=True, text=True, timeout=120, env=dict(os.environ, ASAN_OPTIONS="detect_stack_use_after_return=0"))
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
