@@ -419,6 +419,7 @@ int kv_batch_set_trees(kv_batch* b, int32_t n, const int32_t* offsets, const int
   int64_t units = 0;
   for (int32_t i = 0; i < n; i++) {
     which[i] = !trees || trees[i];
+    if (q_lens[i] < 0 || (which[i] && q_lens[i] > KV_TREE_MAX)) return KV_EINVAL;
     rows = rows || (which[i] && q_lens[i] > 0);
     // (as many workgroups as the request that needs most; more than a launch may have: refused)
     units = std::max<int64_t>(units, which[i] ? (int64_t)q_lens[i] * ((q_lens[i] + 126ll) / 64 * 2) : q_lens[i]);
