@@ -162,6 +162,9 @@ class BatchPlan {
   static constexpr int32_t kRowTile = 16;  // rows of a row tile, but for batches with drafts (BatchShape::row_tile)
   static constexpr int32_t kWeightKeys = 256, kWeightReqs = 16, kScoreKeys = 1024;
 
+  // Tokens of a request at most: the plan and the kernels compute positions up to a step, or kScoreKeys, behind the last one in 32 bits.
+  static constexpr int32_t kMaxTokens = INT32_MAX - kScoreKeys;
+
   bool is_tree(int32_t i) const { return !tree.empty() && tree[i]; }
 
   int set(int32_t n_, const int32_t* offsets, const int32_t* blocks, const int32_t* tokens, const int32_t* q_lens, int32_t num_q_heads,
@@ -170,7 +173,7 @@ class BatchPlan {
     if (n_ && (!offsets || !tokens || !q_lens || offsets[0] < 0)) return KV_EINVAL;
     int64_t rows = 0, keys = 0, table = 0, words = 0;
     for (int32_t i = 0; i < n_; i++) {
-      if (offsets[i + 1] < offsets[i] || tokens[i] < 0 || q_lens[i] < 0) return KV_EINVAL;
+      if (offsets[i + 1] < offsets[i] || tokens[i] < 0 || tokens[i] > kMaxTokens || q_lens[i] < 0) return KV_EINVAL;
       if (q_lens[i] > tokens[i] && !(tokens[i] == 0 && q_lens[i] == 1)) return KV_EINVAL;
       if (trees && trees[i]) {
         if (q_lens[i] > KV_TREE_MAX) return KV_EINVAL;

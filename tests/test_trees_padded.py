@@ -47,3 +47,8 @@ def test_kernels_at_their_edges(edges, name):
 def test_sizes_that_no_launch_could_have(tmp_path):
     r = subprocess.run([_on_mock_hip(tmp_path, "tree_sizes_on_mock_hip")], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_lengths_near_what_32_bits_count(tmp_path):
+    r = subprocess.run([_plain(tmp_path, "lengths_near_2g")], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "lengths ok" in r.stdout, r.stdout + r.stderr
