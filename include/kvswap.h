@@ -535,8 +535,8 @@ int kv_append_axes(kv_batch* b, const kv_append_args* a, int32_t axes, const int
  * rounded once.  For the product with V the weights go into 16 bits: in two terms, which leave out less than 2^-16 of each (in f16: or 2^-34 of
  * the row's largest), or in one, rounded to io_dtype as out is.  One term is for the tokens that a request has for itself where it has more than
  * 16 rows for a KV head (new tokens times query heads: a prompt); all else has two, whatever other requests are in the batch.  In a batch with drafted
- * trees it is for requests with more than 32 rows (16 where heads are not 64 or 128 elements, or blocks no multiple of 16 tokens), which then have one for a
- * prefix, too, if all that share it have as many. */
+ * trees it is for requests with more than 32 rows (16 where heads are not 64 or 128 elements, or blocks no multiple of 16 tokens); if all that share a
+ * prefix draft and have as many, they have one for it, too. */
 typedef struct {
   uint32_t struct_size;
   int32_t layer;

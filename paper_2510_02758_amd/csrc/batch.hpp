@@ -542,13 +542,12 @@ class BatchPlan {
   }
   int64_t most_keys(int32_t B) const { return std::min<int64_t>((int64_t)(kMaxEntries - 1) * B, INT32_MAX / 2) / kStep * kStep; }
 
-  // Are keys that this node's requests share to be weighed as precisely as in row tiles?  With drafts only if one of these has few rows: those that
-  // have many weigh their own keys, and would weigh these without the others, as big tiles do.
+  // Are keys that this node's requests share to be weighed as precisely as in row tiles?  Not if all of them draft and have many rows: these weigh their
+  // own keys, and would weigh these without the others, as big tiles do.  A prompt's are, in a batch with drafts as in one without.
   bool fine(const Node& node) const {
     if (node.reqs.size() < 2) return false;
-    if (tree.empty()) return true;
     for (int32_t i : node.reqs)
-      if ((int64_t)q_len[i] * G <= row_tile_) return true;
+      if (!is_tree(i) || (int64_t)q_len[i] * G <= row_tile_) return true;
     return false;
   }
 

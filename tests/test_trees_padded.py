@@ -52,3 +52,8 @@ def test_sizes_that_no_launch_could_have(tmp_path):
 def test_lengths_near_what_32_bits_count(tmp_path):
     r = subprocess.run([_plain(tmp_path, "lengths_near_2g")], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "lengths ok" in r.stdout, r.stdout + r.stderr
+
+
+def test_prompts_beside_drafts_are_as_precise(tmp_path):
+    r = subprocess.run([_plain(tmp_path, "prompts_beside_drafts")], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "plans ok" in r.stdout, r.stdout + r.stderr
