@@ -49,3 +49,20 @@ def test_a_row_of_no_tree_gives_no_weight_to_an_infinite_key(gpu, dtype, new, sh
     assert (added[:, far] == 0).all()
     slack = (2.0 ** -22 * (1 + np.abs(rw[0])) + wtol[0]) * (1 + new)     # (as in test_gpu_trees.py)
     assert (np.abs(added[:, x] - rw[0]) <= slack).all()
+
+
+def test_paths_of_padded_requests(gpu):
+    """Every row of a tree has an entry of `path`, that of a padded request, too; a request whose new tokens are no tree has none."""
+    import torch
+    lens, q_lens, trees = [40, 0, 9, 30, 0], [4, 1, 0, 3, 1], [True, True, True, False, False]
+    p = Pool(gpu, W.Geometry(2, 2, 64, 16, "bf16", 12), seed=8)
+    rows = _tables(p.rng, 12, lens, 16)
+    p.fill(rows, lens)
+    o, ids = R.csr(rows)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=gpu)  # noqa: E731
+    kv.kv_check(p.batch.set_trees(o, ids, lens, q_lens, 4, dev([-1, 0, 1, -2, -1, 3, 3, 3, 3]), trees))
+    count, nxt, path = dev([-9] * 5), dev([-9] * 5), torch.full((5, 6), -9, dtype=torch.int32, device=gpu)
+    kv.kv_check(p.batch.accept(0, 2, dev([7] * 9), dev([7] * 9), count, path, nxt))
+    assert count.tolist() == [3, 0, 0, 3, 0] and nxt.tolist() == [7, -1, -1, 7, -1]
+    none = [-9] * 6
+    assert path.tolist() == [[0, 1, 2, -1, -9, -9], [-1] + none[1:], none, none, none]
