@@ -66,3 +66,34 @@ def test_paths_of_padded_requests(gpu):
     assert count.tolist() == [3, 0, 0, 3, 0] and nxt.tolist() == [7, -1, -1, 7, -1]
     none = [-9] * 6
     assert path.tolist() == [[0, 1, 2, -1, -9, -9], [-1] + none[1:], none, none, none]
+
+
+@pytest.mark.parametrize("shape", [(2, 128, 8), (3, 72, 6)])
+def test_accepted_rows_between_scales_far_apart(gpu, shape):
+    """A row that comes with a scale beyond 2^128 times that of its new block: what is not 0 becomes +-448, and a 0 stays one."""
+    import torch
+    H, D, B = shape
+    base, new = B, 3 * B
+    p = Pool(gpu, W.Geometry(2, H, D, B, "fp8_e4m3", 8, scales=True), seed=D)
+    rows = _tables(p.rng, 8, [base + new], B)
+    p.fill(rows, [base + new])
+    first, last = int(rows[0][1]), int(rows[0][3])
+    row = 2 * B + 1                                # in the last block; it goes to place 1 of the first with new tokens
+    bits = p.bits()
+    bits[:, :, last, 1, :, ::3] = 0
+    bits[:, :, last, 1, :, 1] = 0x80
+    p.scale[:, :, first] = 1e-30
+    p.scale[:, :, last] = 1e30
+    before = bits.clone()
+    o, ids = R.csr(rows)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device=gpu)  # noqa: E731
+    kv.kv_check(p.batch.set_trees(o, ids, [base + new], [new], H, dev([TR.ROOT] + [0] * (new - 1))))
+    tokens, chosen = dev([0] * new), dev([5] * new)
+    tokens[row] = 5
+    count, nxt, path = dev([0]), dev([0]), torch.zeros(1, new, dtype=torch.int32, device=gpu)
+    kv.kv_check(p.batch.accept(0, 2, tokens, chosen, count, path, nxt))
+    assert count.tolist() == [2] and path[0, :3].tolist() == [0, row, -1]
+    want = before.clone()
+    was = before[:, :, last, 1]
+    want[:, :, first, 1] = torch.where(was & 0x7F == 0, was, was & 0x80 | 0x7E)
+    assert torch.equal(p.bits(), want)
