@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -25,3 +26,10 @@ def gpu():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     return torch.device("cuda:0")
+
+
+@pytest.fixture(autouse=True, scope="module")
+def pools_of_other_modules_are_gone():
+    """Pools that a module's tests left in cycles of references go before the next module's tests begin.  Freeing their memory waits for the device: in the
+    middle of a test that holds a stream back and times the host, the collector would have the host wait for that stream."""
+    gc.collect()
