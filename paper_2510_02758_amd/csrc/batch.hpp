@@ -29,9 +29,9 @@ struct AttnItem {
   int32_t tokens;   // the node's list of tokens
   int32_t row0, rows;
   int32_t part;     // partial row of row0; -1: the rows are finished here
-  // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of 16), key x at 16 score + r score_row + x - score_from.
+  // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of up to row_tile), key x at 16 score + r score_row + x - score_from.
   int32_t score, score_row, score_from;
-  int32_t fine;  // keys that several requests share.  In big tiles their weights are as precise as in row tiles, whatever these requests' number
+  int32_t fine;  // keys that several requests share (not if all of them draft and have many rows).  In big tiles their weights are as precise as in row tiles
   // Of a drafted tree (TreeReq): where the bits of row tree_first begin (-1: no tree's keys), words of a row, their first key.
   int32_t tree, tree_first, tree_words, tree_origin;
 };
@@ -74,7 +74,7 @@ struct BatchShape {
   int row_tile = 16;
   int row_step = 0, big_step = 0;
   int most_heads = 4;  // of a workgroup of row tiles
-  int64_t cached_keys = 0;  // of all heads that the chip's last cache (256 MB) keeps
+  int64_t cached_keys = 0;  // of all heads, in 200 MB: what the chip's last cache (256 MB) keeps beside other data
   int key_rows = 50;    // rows of partial results, of all heads, that cost as much as a workgroup's time for one key
   // A prefix is shared from so many tokens on, by rows of one row tile and by more rows; the latter if all of them together spare `spared` tokens.
   int few_prefix = 64, big_prefix = 64;
@@ -335,7 +335,10 @@ class BatchPlan {
   // anyway, but its partial results have to be joined.  Shared / not, us, 8 heads of 128 in bf16, requests of 40 to 900 tokens of their own: 48 with 128
   // rows behind 2048 127 / 99, behind 4096 199 / 157, behind 8192 346 / 256; 24 with 128 behind 16384 330 / 246; 48 with 192 behind 4096 264 / 227; 48
   // with 96 154 / 149; 64 with 68 152 / 149; 96 with 72 behind 2048 165 / 147; 32 with 160 behind 4096 158 / 159.  With 64 rows and fewer it is worth it: in
-  // fp8 with 40 behind 4096 121 / 158.
+  // fp8 with 40 behind 4096 121 / 158.  Long prefixes, shared / not: 16 with 128 rows (whole tiles) behind 30000 376 / 306, behind 44000 483 / 422, 8 with 256
+  // 498 / 411, 16 with 96 365 / 365; 30 with 80 behind 20000 369 / 349, behind 44000 671 / 770, 60 with 80 724 / 653, 1298 / 1749.  Beyond what the cache
+  // keeps it goes either way: 16 with 128 behind 52000 580 / 481, behind 70000 776 / 621, 40 with 128 behind 60000 2224 / 1883, 16 with 96 547 / 480, 30 with 80
+  // 835 / 1040, 60 with 80 1910 / 2098.
   bool worth_sharing(const std::vector<int32_t>& reqs, int64_t keys, const BatchShape& s) const {
     if (tree.empty() || keys > s.cached_keys) return true;
     for (int32_t i : reqs)
