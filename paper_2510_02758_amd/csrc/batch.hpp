@@ -47,9 +47,10 @@ struct ScoreItem {
 
 // A tree's request, for the kernel that finds out what its rows see.  A row has `words` words of 32 bits, an even number, for the keys from `origin` on
 // (what lies in front of it every row of the tree sees), the first of its request's rows at `word`.  words 0: the new tokens follow one another, or there
-// is nothing that they could see.  tree: the request drafts, also where words is 0 (a padded one).
+// are none; kPadded: a tree of one row where nothing is cached, not even that.
 struct TreeReq {
-  int32_t first, rows, base, word, words, origin, tree;
+  static constexpr int32_t kPadded = -1;
+  int32_t first, rows, base, word, words, origin;
 };
 // The same as a row of the attention needs it; word -1: the row sees the keys in front of its limit.
 struct TreeSight {
@@ -307,7 +308,7 @@ class BatchPlan {
     for (const Node& node : nodes_)
       if (node.reqs.size() == 1 && node.to == len[node.reqs[0]]) from[node.reqs[0]] = node.from;
     for (int32_t i = 0; i < n; i++) {
-      TreeReq r{q_first[i], q_len[i], std::max(len[i] - q_len[i], 0), 0, 0, 0, tree[i]};
+      TreeReq r{q_first[i], q_len[i], std::max(len[i] - q_len[i], 0), 0, tree[i] && q_len[i] ? TreeReq::kPadded : 0, 0};
       if (tree[i] && len[i] && q_len[i]) {
         r.origin = from[i] + (r.base - from[i]) / 64 * 64;
         r.words = (len[i] - r.origin + 63) / 64 * 2;
@@ -316,12 +317,12 @@ class BatchPlan {
       }
       tree_reqs.push_back(r);
       tree_units = std::max(tree_units, r.rows * std::max(r.words, 1));
-      for (int32_t j = 0; j < r.rows; j++) tree_sight.push_back({r.words ? r.word + j * r.words : -1, r.origin});
+      for (int32_t j = 0; j < r.rows; j++) tree_sight.push_back({r.words > 0 ? r.word + j * r.words : -1, r.origin});
     }
     for (AttnItem& it : items) {
       if (it.clear >= it.k1) continue;  // (all of its keys are seen by all rows)
       const TreeReq& r = tree_reqs[tok_req[lists[it.tokens]]];
-      if (r.words) it.tree = r.word, it.tree_first = r.first, it.tree_words = r.words, it.tree_origin = r.origin;
+      if (r.words > 0) it.tree = r.word, it.tree_first = r.first, it.tree_words = r.words, it.tree_origin = r.origin;
     }
     tree_tails_shared = twice([&](auto what) {
       for (int32_t i = 0; i < n; i++)
