@@ -29,7 +29,7 @@ struct AttnItem {
   int32_t tokens;   // the node's list of tokens
   int32_t row0, rows;
   int32_t part;     // partial row of row0; -1: the rows are finished here
-  // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r (of up to row_tile), key x at 16 score + r score_row + x - score_from.
+  // Row tiles: where the products of the tile's rows and keys go if they are wanted: row r, key x at 16 score + r score_row + x - score_from.
   int32_t score, score_row, score_from;
   int32_t fine;  // keys that several requests share (not if all of them draft and have many rows).  In big tiles their weights are as precise as in row tiles
   // Of a drafted tree (TreeReq): where the bits of row tree_first begin (-1: no tree's keys), words of a row, their first key.
