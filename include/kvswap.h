@@ -432,8 +432,8 @@ typedef struct kv_batch kv_batch; /* opaque */
  * allocates as batches grow (it waits on the host for the batch's earlier work where it does).  Two more parts are allocated by the first call that wants them, and
  * from then on by kv_batch_set.  One is kv_attn's with weights, for products: 4 bytes for each of a row tile's up to 16 rows (32 in a batch with
  * drafted trees) and its keys.  Without it, for want of memory or because the first such call is in a capture, they are computed twice.  The other is
- * kv_evict's, for the order of its moves: 8 bytes for each layer, head and some 128 tokens of the longest request, times n.  Without it, and always in a capture, each head's moves are made
- * one after the other. */
+ * kv_evict's, for the order of its moves: 8 bytes for each layer, head and some 128 tokens of the longest request, times n.  Without it, and always
+ * in a capture, each head's moves are made one after the other. */
 int kv_batch_create(kv_pool* p, kv_batch** out);
 /* Waits for the batch's work (for the device, if calls have been captured since the batch was set), then frees it. */
 int kv_batch_destroy(kv_batch* b);
